@@ -138,6 +138,25 @@ AMQ_API amq_status amq_binary_gemm(const uint32_t* Wcodes, const float* Walpha, 
                            const float* bias, float* y, int ldy, void* stream);
 
 /*
+ * The same product with what usually follows it in a layer, in the product's own epilogue:
+ *   y[b][r] = act(sum_i sum_j Walpha[r][i] * xbeta[b][j] * D[b][r][i][j] + bias[r]) + residual[b][r].
+ * activation: AMQ_ACT_NONE, _RELU (max(v, 0)), _GELU (v times the normal distribution function of v), _SILU (v * logistic(v)), _TANH or
+ * _SIGMOID (logistic(v)); anything else: AMQ_ERR_UNSUPPORTED.  residual [batch][ldr] fp32, ldr >= m, or NULL; it may be y itself (with
+ * ldr = ldy), and may not overlap y otherwise.  The other arguments, the kernels and the errors are those of amq_binary_gemm; with
+ * AMQ_ACT_NONE and no residual the results are its results, bit for bit.
+ */
+#define AMQ_ACT_NONE 0
+#define AMQ_ACT_RELU 1
+#define AMQ_ACT_GELU 2
+#define AMQ_ACT_SILU 3
+#define AMQ_ACT_TANH 4
+#define AMQ_ACT_SIGMOID 5
+AMQ_API amq_status amq_binary_gemm_act(const uint32_t* Wcodes, const float* Walpha, int m, int n, int k_w,
+                               const uint32_t* xcodes, const float* xbeta, int batch, int k_a,
+                               const float* bias, int activation, const float* residual, int ldr,
+                               float* y, int ldy, void* stream);
+
+/*
  * The operation Table 6 (Appendix A) times, in one launch: on-line quantization of ONE activation vector (Sec. 4: the
  * hidden state is quantized during inference) followed by the binary matrix-vector product with row-wise quantized
  * weights,
@@ -316,6 +335,77 @@ AMQ_API amq_status amq_lstm_sequence_paper(const uint32_t* Wi_codes, const float
  */
 AMQ_API amq_status amq_log_softmax_argmax(const float* logits, int rows, int n, int ld,
                                   float* logp, int ldp, int32_t* argmax, void* stream);
+
+/*
+ * A paged cache of keys and values held in packed planes: rows as amq_quantize leaves them (k bits, the paper's Eq. 2), so 4 bits a value at k = 4.
+ *   cache_kcodes, cache_vcodes [pages][page_size][heads][k][wpr(d)], cache_kcoeffs, cache_vcoeffs [pages][page_size][heads][k]: DEVICE.
+ *   table   [batch][ld_table] int32, ld_table >= max_pages: the page of tokens [j * page_size, (j + 1) * page_size) of sequence b is
+ *           table[b][j]; entries outside [0, pages) name none, and entries of pages that the length does not reach are not read.
+ *   lengths [batch] int32: tokens of each sequence, the newest included; taken as at least 0 and at most max_pages * page_size by the attention.
+ * 1 <= k <= 4; d up to AMQ_MAX_HEAD_DIM; max_pages * page_size within 31 bits; code pointers 16-byte aligned.
+ *
+ * amq_cache_append: the rows of the `count` newest tokens of every sequence (kcodes [batch][count][heads][k][wpr(d)] and so on, 16-byte aligned
+ * codes) go to positions lengths[b] - count .. lengths[b] - 1.  Rows whose position is negative, lies behind the table or on no page
+ * are left out; of two tokens that go to one slot either may stay.
+ */
+#define AMQ_MAX_HEAD_DIM 128
+AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs, const uint32_t* vcodes, const float* vcoeffs,
+                            uint32_t* cache_kcodes, float* cache_kcoeffs, uint32_t* cache_vcodes, float* cache_vcoeffs,
+                            int pages, int page_size, int heads, int d, int k, const int32_t* table, int ld_table, int max_pages,
+                            const int32_t* lengths, int batch, int count, void* stream);
+
+/*
+ * Attention of the q_len newest tokens of every sequence over the cache (which holds those tokens too).  Query i of sequence b sees tokens
+ * t < lengths[b] - q_len + 1 + i (causal), those on no page left out; q_heads is a multiple of heads, and query head h reads the
+ * keys and values of head h / (q_heads / heads):
+ *   s[t] = scale * (q . khat[t]),  p = softmax(s),  out = sum_t p[t] vhat[t],  khat and vhat the values that the planes stand for.
+ * A query that sees no token gets zeros; one that holds NaN or infinities gets NaN (where it sees a token).
+ *   q   fp32, element (b, i, h, j) at q[b * q_batch + i * q_token + h * q_head + j] (strides in elements).
+ *   out [batch][q_len][q_heads][d] fp32.
+ *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
+ *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
+ * Products with the planes are exact integers on q and p held as 22-bit fixed-point numbers (relative to a query's largest element, and
+ * to the largest weight among 32 tokens); everything else is fp32.  Results repeat bit for bit for the same sizes.
+ */
+AMQ_API size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens);
+AMQ_API amq_status amq_cache_attention(const float* q, long long q_batch, long long q_token, long long q_head,
+                               const uint32_t* cache_kcodes, const float* cache_kcoeffs, const uint32_t* cache_vcodes, const float* cache_vcoeffs,
+                               int pages, int page_size, int heads, int d, int k, const int32_t* table, int ld_table, int max_pages,
+                               const int32_t* lengths, int batch, int q_len, int q_heads, float scale, float* out,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Beam search on the output layer of Eq. 6 (the paper decodes greedily; `beams` = 1 is that): for each of `batch` entries the `beams` best of all
+ * beams * vocab continuations,
+ *   score(b, t) = scores[b] + logits[b][t] - log(sum_u exp(logits[b][u])),
+ * best first, equal scores by the smaller b * vocab + t.  Candidates are compared unrounded (in double); scores_out is rounded to fp32.
+ *   logits       rows entry * beams + b of `ld` >= vocab floats; -inf takes a token out.
+ *   scores       [batch][beams] fp32.  A beam whose score is not finite, or whose logits hold NaN or +inf or nothing but -inf, has no
+ *                continuation: all its pairs score -inf, as do the tokens taken out.  Pairs of -inf are chosen only where there are no others, the
+ *                smallest b * vocab + t first.
+ *   finished     [batch][beams] int32 or NULL: nonzero = the beam has ended.  Its logits are not read; its one continuation is `eos`, at its
+ *                unchanged score.
+ *   eos          token that ends a beam, or -1 (then finished is NULL).
+ *   scores_out [batch][beams] fp32 (may be scores), parents [batch][beams] int32 (b of the choice), tokens [batch][beams] int32,
+ *   finished_out [batch][beams] int32 or NULL (may be finished): the parent's flag, or token = eos.
+ * AMQ_ERR_UNSUPPORTED: beams beyond AMQ_MAX_BEAMS, beams * vocab or 8 * batch beyond 31 bits.
+ */
+#define AMQ_MAX_BEAMS 32
+AMQ_API amq_status amq_beam_select(const float* logits, int ld, int vocab, const float* scores, const int32_t* finished, int eos,
+                           int batch, int beams, float* scores_out, int32_t* parents, int32_t* tokens, int32_t* finished_out,
+                           void* stream);
+
+/*
+ * The states behind the chosen beams: for `count` states (h, c, token histories, rows of a block table, ..) and every entry e, beam b
+ *   dst[i] row (e * beams + b) = src[i] row (e * beams + parents[e][b]),
+ * rows of row_bytes[i] bytes at strides of src_stride[i] and dst_stride[i] bytes (all multiples of 4, addresses too: AMQ_ERR_ALIGNMENT).  dst[i]
+ * may be src[i] with the same stride (in place); it may not overlap any source otherwise.  Parents outside [0, beams) are clamped.  Bytes of
+ * dst between the rows are left as they were.
+ * src, dst, row_bytes, src_stride and dst_stride are HOST arrays of `count` <= AMQ_MAX_STATES; what src and dst hold are DEVICE pointers.
+ */
+#define AMQ_MAX_STATES 8
+AMQ_API amq_status amq_beam_reorder(const void* const* src, void* const* dst, const size_t* row_bytes, const size_t* src_stride,
+                            const size_t* dst_stride, int count, const int32_t* parents, int batch, int beams, void* stream);
 
 /*
  * Greedy decoding with the language model of Eq. 6, one sequence, no host round trip: one kernel launch for all tokens when no

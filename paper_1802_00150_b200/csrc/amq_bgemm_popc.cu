@@ -7,6 +7,7 @@
 // loop independent of them) and four epilogues: raw integer partials, y = sum alpha beta D + bias, and
 // the fused LSTM (Eq. 6) and GRU gate arithmetic.  For the cells a tile holds all gate rows of its
 // hidden units, so the state update needs no second pass over global memory.
+#include "amq_activation.cuh"
 #include "amq_common.cuh"
 
 namespace amq {
@@ -38,6 +39,7 @@ __device__ __forceinline__ uint32_t range_mask(int q, int lo, int hi)
 
 __device__ __forceinline__ float logistic(float v) { return 1.0f / (1.0f + __expf(-v)); }
 
+template <bool POST>
 __global__ void __launch_bounds__(512)
 bgemm_popc_kernel(PopcParams p)
 {
@@ -152,8 +154,14 @@ bgemm_popc_kernel(PopcParams p)
         for (int idx = tid; idx < TM * p.TB; idx += nthreads) {
             const int l = idx / p.TB, bb = idx % p.TB;
             const int row = u0 + l, b = b0 + bb;
-            if (row < a.m && b < a.batch)
-                a.y[(size_t)b * a.ldy + row] = Yt[l * p.TB + bb] + (a.bias ? __ldg(a.bias + row) : 0.0f);
+            if (row < a.m && b < a.batch) {
+                float y = Yt[l * p.TB + bb] + (a.bias ? __ldg(a.bias + row) : 0.0f);
+                if constexpr (POST) {
+                    y = activate(y, a.activation);
+                    if (a.residual) y += __ldcg(a.residual + (size_t)b * a.ldr + row);
+                }
+                a.y[(size_t)b * a.ldy + row] = y;
+            }
         }
     } else if (a.epilogue == EPI_LSTM) {
         const int H = a.H;
@@ -238,7 +246,8 @@ amq_status launch_binary_gemm(const GemmArgs& a, cudaStream_t st)
     const size_t smem = (size_t)(ab_words > p_words ? ab_words : p_words) * 4 + (size_t)2 * TM * p.TB * 4;
     dim3 grid((unsigned)((p.units + p.UT - 1) / p.UT), (unsigned)((a.batch + p.TB - 1) / p.TB));
     if (grid.y > 65535u) return AMQ_ERR_UNSUPPORTED;
-    bgemm_popc_kernel<<<grid, threads, smem, st>>>(p);
+    auto kernel = a.post ? bgemm_popc_kernel<true> : bgemm_popc_kernel<false>;
+    kernel<<<grid, threads, smem, st>>>(p);
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;
 }
@@ -285,6 +294,21 @@ amq_status amq_binary_gemm(const uint32_t* Wcodes, const float* Walpha, int m, i
     amq::GemmArgs a{};
     const amq_status s = amq::product_call(Wcodes, Walpha, m, n, k_w, xcodes, xbeta, batch, k_a, bias, y, ldy, &a);
     if (s != AMQ_OK || m == 0 || batch == 0) return s;
+    return amq::launch_binary_gemm(a, (cudaStream_t)stream);
+}
+
+amq_status amq_binary_gemm_act(const uint32_t* Wcodes, const float* Walpha, int m, int n, int k_w,
+                               const uint32_t* xcodes, const float* xbeta, int batch, int k_a,
+                               const float* bias, int activation, const float* residual, int ldr, float* y, int ldy, void* stream)
+{
+    amq::GemmArgs a{};
+    const amq_status s = amq::product_call(Wcodes, Walpha, m, n, k_w, xcodes, xbeta, batch, k_a, bias, y, ldy, &a);
+    if (s != AMQ_OK) return s;
+    if (residual && (ldr < m || (residual == y && ldr != ldy && batch > 1))) return AMQ_ERR_INVALID_ARG;
+    if (activation < AMQ_ACT_NONE || activation > AMQ_ACT_SIGMOID) return AMQ_ERR_UNSUPPORTED;
+    if (m == 0 || batch == 0) return AMQ_OK;
+    a.post = activation != AMQ_ACT_NONE || residual;
+    a.activation = activation; a.residual = residual; a.ldr = ldr;
     return amq::launch_binary_gemm(a, (cudaStream_t)stream);
 }
 

@@ -7,6 +7,7 @@
 // MMAs.  That product took 59.8 us with a constant of every operand row added back in the epilogue (twice the instructions, and its
 // loads kept the load/store unit busy) and the polling warp on the issuing warp's scheduler; 52.5 us now (behind a flush of L2 65.6 and 59.4).  Outputs leave through shared
 // memory as 16-byte pieces.
+#include "amq_activation.cuh"
 #include "amq_resident.cuh"
 
 namespace amq {
@@ -17,6 +18,7 @@ struct ResGemmParams {
     ResProblem p;
     const uint32_t* xcodes; const float* xbeta; const float* bias;
     float* y; int ldy;
+    int activation; const float* residual; int ldr;     // POST
     int mtiles, blocks;         // tiles of 128 rows, blocks of TB vectors
     int b_bytes;                // expanded activation operand
     int early_weights;          // the kernel before does not write the weights: they may be fetched before it is through
@@ -30,10 +32,10 @@ __host__ __device__ constexpr int res_ng(int k_a) { return k_a <= 2 ? 2 : 1; }
 
 using R = ResRoles<3, 16, 3>;
 
-// VEC: every row of the result starts on 16 bytes.  (Two kernels, not two paths in one: the registers and instructions of all the roles of a
+// VEC: every row of the result (and of the residual) starts on 16 bytes.  (Two kernels, not two paths in one: the registers and instructions of all the roles of a
 // kernel of 1024 threads count for each role.  Without VEC a thread stores its four rows one by one; contiguous 128-byte stores, or
 // 16-byte pieces shifted against the rows, were slower at most sizes: up to 35 % for rows of 2000 and more.)
-template <int KA, bool VEC>
+template <int KA, bool VEC, bool POST>
 __global__ void __launch_bounds__(R::THREADS, 1)
 bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
 {
@@ -187,6 +189,22 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
                 for (int e = warp - R::MMA_WARP - 1; e < last; e += R::OUT_WARPS) {
                     float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
                     v.x += bias.x; v.y += bias.y; v.z += bias.z; v.w += bias.w;
+                    if constexpr (POST) {
+                        float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (a.residual) {
+                            const float* res = a.residual + (size_t)(b0 + e) * a.ldr + row;
+                            if (vec) {
+                                r = __ldcg(reinterpret_cast<const float4*>(res));
+                            } else {
+                                if (row < p.units) r.x = __ldcg(res);
+                                if (row + 1 < p.units) r.y = __ldcg(res + 1);
+                                if (row + 2 < p.units) r.z = __ldcg(res + 2);
+                                if (row + 3 < p.units) r.w = __ldcg(res + 3);
+                            }
+                        }
+                        v.x = activate(v.x, a.activation) + r.x; v.y = activate(v.y, a.activation) + r.y;
+                        v.z = activate(v.z, a.activation) + r.z; v.w = activate(v.w, a.activation) + r.w;
+                    }
                     float* out = a.y + (size_t)(b0 + e) * a.ldy + row;
                     if (vec) {
                         *reinterpret_cast<float4*>(out) = v;
@@ -247,15 +265,16 @@ bool plan(const GemmArgs& g, int sms, ResGemmPlan* out)
     out->grid = (int)(total < sms ? total : sms);
     out->smem = res_smem_bytes(a.p) + (size_t)a.p.TB * Y_LD * 4;
     a.early_weights = !g.from_entry;
-    out->vec_out = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && g.ldy % 4 == 0;
+    a.activation = g.activation; a.residual = g.residual; a.ldr = g.ldr;
+    out->vec_out = aligned16(g.y) && g.ldy % 4 == 0 && (!g.residual || (aligned16(g.residual) && g.ldr % 4 == 0));
     out->a = a;
     return true;
 }
 
-template <int KA>
+template <int KA, bool POST>
 amq_status launch(const ResGemmPlan& pl, bool overlap, cudaStream_t st)
 {
-    auto kernel = pl.vec_out ? bgemm_resident_kernel<KA, true> : bgemm_resident_kernel<KA, false>;
+    auto kernel = pl.vec_out ? bgemm_resident_kernel<KA, true, POST> : bgemm_resident_kernel<KA, false, POST>;
     AMQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.smem));
     AMQ_CUDA_TRY(launch_kernel(kernel, dim3((unsigned)pl.grid), dim3(R::THREADS), pl.smem, st, overlap, pl.a));
     AMQ_LAUNCH_CHECK();
@@ -284,11 +303,12 @@ amq_status launch_binary_gemm_resident(const GemmArgs& g, cudaStream_t st)
     if (!plan(g, res_sm_count(), &pl)) return AMQ_ERR_UNSUPPORTED;
     amq_status s = tc_status_word(&pl.a.status);
     if (s != AMQ_OK) return s;
+    const bool overlap = g.overlap_with_previous || g.from_entry;
     switch (g.k_a) {
-        case 1: return launch<1>(pl, g.overlap_with_previous || g.from_entry, st);
-        case 2: return launch<2>(pl, g.overlap_with_previous || g.from_entry, st);
-        case 3: return launch<3>(pl, g.overlap_with_previous || g.from_entry, st);
-        case 4: return launch<4>(pl, g.overlap_with_previous || g.from_entry, st);
+        case 1: return g.post ? launch<1, true>(pl, overlap, st) : launch<1, false>(pl, overlap, st);
+        case 2: return g.post ? launch<2, true>(pl, overlap, st) : launch<2, false>(pl, overlap, st);
+        case 3: return g.post ? launch<3, true>(pl, overlap, st) : launch<3, false>(pl, overlap, st);
+        case 4: return g.post ? launch<4, true>(pl, overlap, st) : launch<4, false>(pl, overlap, st);
     }
     return AMQ_ERR_UNSUPPORTED;
 }

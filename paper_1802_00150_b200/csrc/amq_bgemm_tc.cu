@@ -42,6 +42,7 @@
 // double-buffered in tensor memory, dedicated epilogue warps, so that the epilogue of a tile overlaps the main
 // loop of the next).  Both may be launched as programmatic dependents of the kernel that produces the
 // activation planes: they set themselves up and fetch weight rows, then wait for it.
+#include "amq_activation.cuh"
 #include "amq_common.cuh"
 #include "amq_tcgen05.cuh"
 
@@ -403,6 +404,7 @@ __device__ __forceinline__ void epilogue_tmem_to_smem(const TcParams& p, uint32_
 }
 
 // Epilogue, second half: sum the k_w planes of each weight row, bias, gates; `nthreads` threads numbered `tid`.
+template <bool POST>
 __device__ __forceinline__ void epilogue_smem_to_global(const TcParams& p, const float* Yt, int u0, int b0, int tid, int nthreads)
 {
     // thread -> (row or unit, every `bstep`-th batch entry): one division per thread, none per output
@@ -431,10 +433,23 @@ __device__ __forceinline__ void epilogue_smem_to_global(const TcParams& p, const
                 if (k_w > 1) { const float4 v = *reinterpret_cast<const float4*>(y0 + ldy + b4); s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; }
                 if (k_w > 2) { const float4 v = *reinterpret_cast<const float4*>(y0 + 2 * ldy + b4); s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; }
                 if (k_w > 3) { const float4 v = *reinterpret_cast<const float4*>(y0 + 3 * ldy + b4); s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; }
-                out[(size_t)b4 * a.ldy] = bias + s.x;
-                if (b4 + 1 < bend) out[(size_t)(b4 + 1) * a.ldy] = bias + s.y;
-                if (b4 + 2 < bend) out[(size_t)(b4 + 2) * a.ldy] = bias + s.z;
-                if (b4 + 3 < bend) out[(size_t)(b4 + 3) * a.ldy] = bias + s.w;
+                s.x += bias; s.y += bias; s.z += bias; s.w += bias;
+                if constexpr (POST) {
+                    float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);         // on its way while the activation is computed
+                    if (a.residual) {
+                        const float* res = a.residual + (size_t)(b0 + b4) * a.ldr + row;
+                        r.x = __ldcg(res);
+                        if (b4 + 1 < bend) r.y = __ldcg(res + a.ldr);
+                        if (b4 + 2 < bend) r.z = __ldcg(res + 2 * (size_t)a.ldr);
+                        if (b4 + 3 < bend) r.w = __ldcg(res + 3 * (size_t)a.ldr);
+                    }
+                    s.x = activate(s.x, a.activation) + r.x; s.y = activate(s.y, a.activation) + r.y;
+                    s.z = activate(s.z, a.activation) + r.z; s.w = activate(s.w, a.activation) + r.w;
+                }
+                out[(size_t)b4 * a.ldy] = s.x;
+                if (b4 + 1 < bend) out[(size_t)(b4 + 1) * a.ldy] = s.y;
+                if (b4 + 2 < bend) out[(size_t)(b4 + 2) * a.ldy] = s.z;
+                if (b4 + 3 < bend) out[(size_t)(b4 + 3) * a.ldy] = s.w;
             }
         } else if (a.epilogue == EPI_LSTM) {
             const int H = a.H, u = u0 + item;
@@ -485,7 +500,7 @@ __device__ __forceinline__ void epilogue_smem_to_global(const TcParams& p, const
     }
 }
 
-template <int KA, bool FP4>
+template <int KA, bool FP4, bool POST>
 __global__ void __launch_bounds__(MAX_THREADS, 1)
 bgemm_tc_kernel(TcParams p)
 {
@@ -768,7 +783,7 @@ bgemm_tc_kernel(TcParams p)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"((uint32_t)p.tmem_cols) : "memory");
     if (a.epilogue == EPI_DOTS) return;
 
-    epilogue_smem_to_global(p, Yt, u0, b0, tid, nthreads);
+    epilogue_smem_to_global<POST>(p, Yt, u0, b0, tid, nthreads);
 }
 
 // The persistent form of the kernel, for problems of more tiles than the GPU has SMs: one CTA per SM walks over
@@ -777,7 +792,7 @@ bgemm_tc_kernel(TcParams p)
 // expansion and the MMAs of the next one (bound by shared-memory traffic).  The stage pipeline runs on across
 // tiles; "accumulator full" barriers are signalled by tcgen05.commit after the last MMA of a tile,
 // "accumulator empty" ones by the epilogue warps after their last read of tensor memory.
-template <int KA, bool FP4>
+template <int KA, bool FP4, bool POST>
 __global__ void __launch_bounds__(MAX_THREADS, 1)
 bgemm_tc_persistent_kernel(TcParams p)
 {
@@ -1071,7 +1086,7 @@ bgemm_tc_persistent_kernel(TcParams p)
             epi_bar(nth_e);                                         // the staging array is complete, the coefficients are read
             const bool more = tile + tile_step < ntiles;
             if (more) coef_load(tile + tile_step);
-            epilogue_smem_to_global(p, Yt, u0, b0, tid_e, nth_e);
+            epilogue_smem_to_global<POST>(p, Yt, u0, b0, tid_e, nth_e);
             if (more) coef_store();                                 // (visible to the others after the next tile's barrier)
             __syncwarp();
         }
@@ -1232,11 +1247,11 @@ bool plan(const GemmArgs& a, TcPlan* out, int sms = 0)
     return out->grid.y <= 65535u && out->smem <= 227 * 1024;
 }
 
-template <int KA>
+template <int KA, bool POST>
 amq_status launch_ka(const TcPlan& pl, cudaStream_t st)
 {
-    auto kernel = pl.persistent ? (pl.p.fp4 ? bgemm_tc_persistent_kernel<KA, true> : bgemm_tc_persistent_kernel<KA, false>)
-                                : (pl.p.fp4 ? bgemm_tc_kernel<KA, true> : bgemm_tc_kernel<KA, false>);
+    auto kernel = pl.persistent ? (pl.p.fp4 ? bgemm_tc_persistent_kernel<KA, true, POST> : bgemm_tc_persistent_kernel<KA, false, POST>)
+                                : (pl.p.fp4 ? bgemm_tc_kernel<KA, true, POST> : bgemm_tc_kernel<KA, false, POST>);
     AMQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.smem));
     if (pl.p.a.overlap_with_previous || pl.p.a.from_entry) {
         cudaLaunchConfig_t cfg{};
@@ -1303,10 +1318,10 @@ amq_status launch_binary_gemm_tc(const GemmArgs& a, cudaStream_t st)
     TcPlan pl;
     if (!plan(a, &pl)) return AMQ_ERR_UNSUPPORTED;
     switch (a.k_a) {
-        case 1: return launch_ka<1>(pl, st);
-        case 2: return launch_ka<2>(pl, st);
-        case 3: return launch_ka<3>(pl, st);
-        case 4: return launch_ka<4>(pl, st);
+        case 1: return a.post ? launch_ka<1, true>(pl, st) : launch_ka<1, false>(pl, st);
+        case 2: return a.post ? launch_ka<2, true>(pl, st) : launch_ka<2, false>(pl, st);
+        case 3: return a.post ? launch_ka<3, true>(pl, st) : launch_ka<3, false>(pl, st);
+        case 4: return a.post ? launch_ka<4, true>(pl, st) : launch_ka<4, false>(pl, st);
     }
     return AMQ_ERR_UNSUPPORTED;
 }

@@ -98,8 +98,9 @@ struct GemmArgs {
     int epilogue;
     // EPI_DOTS
     int32_t* D;
-    // EPI_Y
+    // EPI_Y; `post`: y = activation(product + bias) + residual[b * ldr + r] (residual may be null, or y itself)
     float* y; int ldy;
+    bool post; int activation; const float* residual; int ldr;
     // EPI_LSTM / EPI_GRU
     int I, H;
     const float* h_in; const float* c_in; float* h_out; float* c_out;
