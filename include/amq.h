@@ -342,13 +342,14 @@ AMQ_API amq_status amq_log_softmax_argmax(const float* logits, int rows, int n, 
  *   table   [batch][ld_table] int32, ld_table >= max_pages: the page of tokens [j * page_size, (j + 1) * page_size) of sequence b is
  *           table[b][j]; entries outside [0, pages) name none, and entries of pages that the length does not reach are not read.
  *   lengths [batch] int32: tokens of each sequence, the newest included; taken as at least 0 and at most max_pages * page_size by the attention.
- * 1 <= k <= 4; d up to AMQ_MAX_HEAD_DIM; max_pages * page_size within 31 bits; code pointers 16-byte aligned.
+ * 1 <= k <= 4; d up to AMQ_MAX_HEAD_DIM; max_pages * page_size up to AMQ_MAX_TOKENS; code pointers 16-byte aligned.
  *
  * amq_cache_append: the rows of the `count` newest tokens of every sequence (kcodes [batch][count][heads][k][wpr(d)] and so on, 16-byte aligned
  * codes) go to positions lengths[b] - count .. lengths[b] - 1.  Rows whose position is negative, lies behind the table or on no page
  * are left out; of two tokens that go to one slot either may stay.
  */
 #define AMQ_MAX_HEAD_DIM 128
+#define AMQ_MAX_TOKENS 0x7fffff00   /* of a sequence: max_pages * page_size */
 AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs, const uint32_t* vcodes, const float* vcoeffs,
                             uint32_t* cache_kcodes, float* cache_kcoeffs, uint32_t* cache_vcodes, float* cache_vcoeffs,
                             int pages, int page_size, int heads, int d, int k, const int32_t* table, int ld_table, int max_pages,

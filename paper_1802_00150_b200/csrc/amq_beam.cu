@@ -7,10 +7,10 @@
 // than fp32 rounding of a score of -20 (2e-6), those of one beam never change places.
 //
 // A cluster of eight CTAs takes a batch entry; CTA c reads the eighth c of every beam's row, so any number of beams is balanced, and one entry
-// alone still has eight SMs.  Each thread holds CHUNK_PER_THREAD logits of a chunk in registers (and the next chunk is on its way: loads are one
-// word a lane, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's sum does not depend on where it
-// starts: equal rows get equal sums).  The K-th largest of a warp's 32 lane maxima is a lower bound of the K-th largest of the row; the
-// CTA's best such bound leaves little more than K candidates to write down.
+// alone still has eight SMs.  A group of 256 threads holds a beam's eighth in registers (in pieces where it has more than 6144 words), one word a
+// lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's sum does not depend
+// on where it starts: equal rows get equal sums.  The K-th largest of the maxima of 32 groups of eight lanes is a lower bound of the eighth's K-th
+// largest logit, and little more than K logits reach it; those are written down.
 #include <cooperative_groups.h>
 
 #include "amq_common.cuh"
@@ -21,10 +21,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int SLICES = 8;               // CTAs of a cluster
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;            // of a group; a CTA has one to four, each with beams of its own
 constexpr int WARPS = THREADS / 32;
-constexpr int PER_THREAD = 8;
-constexpr int CHUNK = THREADS * PER_THREAD;
+constexpr int MAX_GROUPS = 4;
 constexpr int CAP = 128;                // candidates kept of a beam's slice; where more pass the bound (ties), the slice is searched again
 
 struct SelectParams {
@@ -51,7 +50,6 @@ struct SelectSmem {
     WarpSum* sums;
     unsigned long long* best;           // [beams][beams], 0 where there are fewer
     unsigned long long* list;           // [beams][CAP] as found
-    uint32_t* bound;                    // [beams] ordered lower bound of the K-th largest
     int* count;                         // [beams]
     // rank 0: all candidates by score
     double* total;                      // [SLICES * beams * beams]
@@ -68,11 +66,10 @@ __host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* ba
     char* total = take(8ull * SLICES * beams * beams);      // (the lists are read before the scores are written)
     char* pair = take(4ull * SLICES * beams * beams);
     char* list = take(8ull * CAP * beams);
-    char* bound = take(4ull * beams);
     char* count = take(4ull * beams);
     if (s) {
         s->sums = reinterpret_cast<WarpSum*>(sums); s->best = reinterpret_cast<unsigned long long*>(best);
-        s->list = reinterpret_cast<unsigned long long*>(list); s->bound = reinterpret_cast<uint32_t*>(bound);
+        s->list = reinterpret_cast<unsigned long long*>(list);
         s->count = reinterpret_cast<int*>(count); s->total = reinterpret_cast<double*>(total); s->pair = reinterpret_cast<int*>(pair);
     }
     return off;
@@ -83,17 +80,22 @@ __device__ __forceinline__ uint32_t redux_max(uint32_t v) { return __reduce_max_
 // (score, pair) a before b
 __device__ __forceinline__ bool before(double a, int ai, double b, int bi) { return a > b || (a == b && ai < bi); }
 
-__global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(THREADS)
+// PT: words of a thread and piece
+template <int PT>
+__global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(THREADS * MAX_GROUPS)
 beam_select_kernel(SelectParams p)
 {
+    constexpr int CHUNK = THREADS * PT;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ float s_score[AMQ_MAX_BEAMS];
     __shared__ int s_done[AMQ_MAX_BEAMS];
     __shared__ double s_lse[AMQ_MAX_BEAMS];
+    __shared__ uint32_t s_maxima[MAX_GROUPS][2][32];
     __shared__ double s_cut; __shared__ int s_cut_pair; __shared__ int s_found;
     __shared__ double s_chosen[AMQ_MAX_BEAMS]; __shared__ int s_chosen_pair[AMQ_MAX_BEAMS];
     cg::cluster_group cluster = cg::this_cluster();
-    const int K = p.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int K = p.beams, tid = threadIdx.x, nthreads = blockDim.x, lane = tid & 31;
+    const int groups = nthreads / THREADS, group = tid / THREADS, at_group = tid % THREADS, warp = at_group >> 5;
     SelectSmem s;
     select_smem(K, &s, smem_raw);
     const int rank = (int)cluster.block_rank(), entry = blockIdx.x / SLICES;
@@ -101,67 +103,72 @@ beam_select_kernel(SelectParams p)
     const size_t row0 = (size_t)entry * K;
 
     grid_dependency_wait();             // logits, scores and flags may come from the preceding kernel of the stream
-    for (int b = tid; b < K; b += THREADS) {
+    for (int b = tid; b < K; b += nthreads) {
         s_score[b] = p.scores[row0 + b];
         s_done[b] = p.finished ? p.finished[row0 + b] != 0 : 0;
-        s.bound[b] = 0;                 // below every logit that counts
         s.count[b] = 0;
     }
     __syncthreads();
 
     // a row is read where its candidates can have a score
     auto open = [&](int b) { return !s_done[b] && isfinite(s_score[b]); };
-    auto next_open = [&](int b) { while (b < K && !open(b)) ++b; return b; };
     const int chunks = hi > lo ? (hi - lo + CHUNK - 1) / CHUNK : 0;
-    auto load = [&](float (&v)[PER_THREAD], int b, int c) {
+    float cur[PT];
+    auto load = [&](int b, int c) {
         const float* z = p.logits + (row0 + b) * p.ld;
-        const int at = lo + c * CHUNK + tid;
+        const int first = lo + c * CHUNK + at_group;
 #pragma unroll
-        for (int i = 0; i < PER_THREAD; ++i) v[i] = at + i * THREADS < hi ? __ldcg(z + at + i * THREADS) : -INFINITY;
+        for (int i = 0; i < PT; ++i) cur[i] = first + i * THREADS < hi ? __ldcg(z + first + i * THREADS) : -INFINITY;
     };
+    auto next_open = [&](int b) { while (b < K && !open(b)) b += groups; return b; };
 
-    for (int b = tid; b < K; b += THREADS)
+    for (int b = tid; b < K; b += nthreads)
         if (chunks == 0 || !open(b))
             for (int w = 0; w < WARPS; ++w) s.sums[b * WARPS + w] = {-INFINITY, 0.0f};
-    int b = chunks ? next_open(0) : K, c = 0;
-    float cur[PER_THREAD], nxt[PER_THREAD];
-    if (b < K) load(cur, b, 0);
+    int b = chunks ? next_open(group) : K, c = 0, buffer = 0;
+    if (b < K) load(b, 0);
     float m = -INFINITY, sum = 0.0f;
+    uint32_t bound = 0;                 // below every logit that counts
     while (b < K) {
-        int nb = b, nc = c + 1;
-        if (nc == chunks) { nc = 0; nb = next_open(b + 1); }
-        if (nb < K) load(nxt, nb, nc);
         // largest and sum of exponentials of this thread's share so far
         float top = cur[0];
 #pragma unroll
-        for (int i = 1; i < PER_THREAD; ++i) top = fmaxf(top, cur[i]);
+        for (int i = 1; i < PT; ++i) top = fmaxf(top, cur[i]);
+        const uint32_t v = top > -INFINITY ? ordered(top) : 0u;
+        uint32_t eight = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
+        eight = max(eight, __shfl_xor_sync(0xffffffffu, eight, 2));
+        eight = max(eight, __shfl_xor_sync(0xffffffffu, eight, 4));
+        if ((lane & 7) == 0) s_maxima[group][buffer][at_group >> 3] = eight;
         const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.0f : m_new;
         sum *= __expf(m - ref);
 #pragma unroll
-        for (int i = 0; i < PER_THREAD; ++i) sum += __expf(cur[i] - ref);
+        for (int i = 0; i < PT; ++i) sum += __expf(cur[i] - ref);
         m = m_new;
-        // the warp's bound, where it can raise the CTA's: the K-th largest lane maximum
-        uint32_t v = top > -INFINITY ? ordered(top) : 0u, kth = 0;
-        if (redux_max(v) > *(volatile uint32_t*)&s.bound[b]) {
-            uint32_t left = v;
+        asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
+        // (the two buffers in turn: who writes one again has passed the barrier behind everybody's reading of it)
+        uint32_t left = s_maxima[group][buffer][lane];
+        buffer ^= 1;
+        if (redux_max(left) > bound) {
+            uint32_t kth = 0;
             for (int r = 0; r < K; ++r) {
                 kth = redux_max(left);
                 const uint32_t has = __ballot_sync(0xffffffffu, left == kth);
                 if (lane == __ffs(has) - 1) left = 0u;
             }
-            if (lane == 0 && kth) atomicMax(&s.bound[b], kth);
+            bound = max(bound, kth);
         }
-        __syncthreads();
-        const uint32_t bound = *(volatile uint32_t*)&s.bound[b];
-        if (v >= bound && v) {
+        if (v && v >= bound) {
 #pragma unroll
-            for (int i = 0; i < PER_THREAD; ++i) {
+            for (int i = 0; i < PT; ++i) {
                 if (cur[i] > -INFINITY && ordered(cur[i]) >= bound) {
-                    const int at = atomicAdd(&s.count[b], 1);
-                    if (at < CAP) s.list[b * CAP + at] = candidate(cur[i], lo + c * CHUNK + tid + i * THREADS);
+                    const int to = atomicAdd(&s.count[b], 1);
+                    if (to < CAP) s.list[b * CAP + to] = candidate(cur[i], lo + c * CHUNK + at_group + i * THREADS);
                 }
             }
         }
+        int nb = b, nc = c + 1;
+        if (nc == chunks) { nc = 0; nb = next_open(b + groups); }
+        if (nb < K) load(nb, nc);
         if (nb != b) {                  // the row is through: the warp's share of its sum
             const uint32_t wm = redux_max(m > -INFINITY ? ordered(m) : 0u);
             const float M = wm ? from_ordered(wm) : -INFINITY;
@@ -169,16 +176,14 @@ beam_select_kernel(SelectParams p)
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
             if (lane == 0) s.sums[b * WARPS + warp] = {M, t};
-            m = -INFINITY; sum = 0.0f;
+            m = -INFINITY; sum = 0.0f; bound = 0;
         }
-#pragma unroll
-        for (int i = 0; i < PER_THREAD; ++i) cur[i] = nxt[i];
         b = nb; c = nc;
     }
     __syncthreads();
 
     // the K best of each beam's slice, in order: a candidate's place is the number of candidates before it
-    for (int q = warp; q < K; q += WARPS) {
+    for (int q = tid >> 5; q < K; q += nthreads >> 5) {
         const int n = s.count[q];
         unsigned long long* best = s.best + (size_t)q * K;
         if (n <= CAP) {
@@ -213,7 +218,7 @@ beam_select_kernel(SelectParams p)
     cluster.sync();
     if (rank == 0) {
         // log-sum-exp of each row, from the 64 warps' shares, in double
-        for (int q = warp; q < K; q += WARPS) {
+        for (int q = tid >> 5; q < K; q += nthreads >> 5) {
             float wm[2], ws[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -235,7 +240,7 @@ beam_select_kernel(SelectParams p)
         __syncthreads();
         // every candidate's score; a beam's lists lie one behind the other, [beam][slice][place]
         const int all = K * SLICES * K;
-        for (int i = tid; i < all; i += THREADS) {
+        for (int i = tid; i < all; i += nthreads) {
             const int q = i / (SLICES * K), slice = i / K % SLICES, r = i % K;
             double total = -INFINITY;
             int pair = 0x7fffffff;
@@ -258,7 +263,7 @@ beam_select_kernel(SelectParams p)
 
     // The K-th best of the lists' heads bounds what can be chosen: at most K lists reach it.  (Heads without a candidate are all alike and last.)
     const int heads = K * SLICES;
-    for (int i = tid; i < heads; i += THREADS) {
+    for (int i = tid; i < heads; i += nthreads) {
         const double mine = s.total[i * K];
         const int pair = s.pair[i * K];
         if (pair == 0x7fffffff) continue;
@@ -270,7 +275,7 @@ beam_select_kernel(SelectParams p)
     // candidates at or before the bound, written down (over the lists of this CTA, which have been read)
     double* kept = reinterpret_cast<double*>(s.best);                       // [K * K] doubles
     int* kept_pair = reinterpret_cast<int*>(s.list);                        // [K * CAP * 2] words: K * K fit
-    for (int i = tid; i < K * SLICES * K; i += THREADS) {
+    for (int i = tid; i < K * SLICES * K; i += nthreads) {
         const int pair = s.pair[i];
         if (pair == 0x7fffffff || before(s_cut, s_cut_pair, s.total[i], pair)) continue;
         const int at = atomicAdd(&s_found, 1);
@@ -278,7 +283,7 @@ beam_select_kernel(SelectParams p)
     }
     __syncthreads();
     const int found = s_found;
-    for (int i = tid; i < found; i += THREADS) {
+    for (int i = tid; i < found; i += nthreads) {
         int place = 0;
         for (int j = 0; j < found; ++j) place += before(kept[j], kept_pair[j], kept[i], kept_pair[i]);
         if (place < K) { s_chosen[place] = kept[i]; s_chosen_pair[place] = kept_pair[i]; }
@@ -303,6 +308,31 @@ beam_select_kernel(SelectParams p)
         p.tokens[row0 + tid] = token;
         if (p.finished_out) p.finished_out[row0 + tid] = (s_done[parent] || token == p.eos) ? 1 : 0;
     }
+}
+
+template <int PT>
+amq_status launch_select_as(const SelectParams& p, int batch, int groups, cudaStream_t st)
+{
+    const size_t smem = select_smem(p.beams, nullptr, nullptr);
+    AMQ_CUDA_TRY(cudaFuncSetAttribute(beam_select_kernel<PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    AMQ_CUDA_TRY(launch_kernel(beam_select_kernel<PT>, dim3((unsigned)(batch * SLICES)), dim3((unsigned)(THREADS * groups)), smem, st, true, p));
+    AMQ_LAUNCH_CHECK();
+    return AMQ_OK;
+}
+
+amq_status launch_select(const SelectParams& p, int batch, cudaStream_t st)
+{
+    // beams at a time: as many as leave the CTAs of all entries on the GPU at once
+    int groups = batch * SLICES <= 148 ? MAX_GROUPS : batch * SLICES <= 296 ? 2 : 1;
+    if (groups > p.beams) groups = p.beams;
+    const int slice = (p.vocab + SLICES - 1) / SLICES, pieces = (slice + THREADS * 24 - 1) / (THREADS * 24);
+    const int words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
+    if (words <= 2) return launch_select_as<2>(p, batch, groups, st);
+    if (words <= 5) return launch_select_as<5>(p, batch, groups, st);
+    if (words <= 8) return launch_select_as<8>(p, batch, groups, st);
+    if (words <= 12) return launch_select_as<12>(p, batch, groups, st);
+    if (words <= 16) return launch_select_as<16>(p, batch, groups, st);
+    return launch_select_as<24>(p, batch, groups, st);
 }
 
 // ---- reordering ------------------------------------------------------------------------------------------------------
@@ -373,12 +403,7 @@ amq_status amq_beam_select(const float* logits, int ld, int vocab, const float* 
     if (batch == 0) return AMQ_OK;
     if (!logits || !scores || !scores_out || !parents || !tokens) return AMQ_ERR_INVALID_ARG;
     amq::SelectParams p{logits, ld, vocab, scores, finished, eos, beams, scores_out, parents, tokens, finished_out};
-    const size_t smem = amq::select_smem(beams, nullptr, nullptr);
-    AMQ_CUDA_TRY(cudaFuncSetAttribute(amq::beam_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    AMQ_CUDA_TRY(amq::launch_kernel(amq::beam_select_kernel, dim3((unsigned)(batch * amq::SLICES)), dim3(amq::THREADS), smem, (cudaStream_t)stream,
-                                    true, p));
-    AMQ_LAUNCH_CHECK();
-    return AMQ_OK;
+    return amq::launch_select(p, batch, (cudaStream_t)stream);
 }
 
 amq_status amq_beam_reorder(const void* const* src, void* const* dst, const size_t* row_bytes, const size_t* src_stride, const size_t* dst_stride,

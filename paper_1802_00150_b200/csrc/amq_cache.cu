@@ -61,64 +61,409 @@ struct AttentionParams {
     CacheView c;
     const float* q; long long q_batch, q_token, q_head;
     int q_len, q_heads, group;
+    int rows, row_blocks;               // query rows of a key head: q_len * group, in blocks of ROWS
+    int splits;                         // shares of a sequence's tokens
+    bool wide;                          // coefficient rows on their own size (4, 8 or 16 bytes)
     float scale;
     float* out;
+    float* part; float2* part_ml;       // splits > 1: unnormalised results and {maximum, sum} of each share, [row][split]
 };
 
-constexpr int DPL = AMQ_MAX_HEAD_DIM / 32;      // dimensions of a lane
+constexpr int WARPS = 4;
+constexpr int TILE = 32;                // tokens
+constexpr int STAGES = 3;
+constexpr int ROWS = 4;                 // query rows of a CTA
+constexpr float MAGIC = 12582912.0f;    // 1.5 2^23: a float of this size holds an integer of 22 bits in its low bits
+constexpr int MAGIC_BITS = 0x4B400000;
 
-// one CTA per query row; its warps take every fourth token
-__global__ void __launch_bounds__(128)
+// chunks (16 bytes: a plane of up to 128 bits) and coefficients of a token in shared memory; four for three
+__host__ __device__ constexpr int pitch(int k) { return k == 3 ? 4 : k; }
+template <int K> struct Stage {
+    uint4 k[TILE * pitch(K)], v[TILE * pitch(K)];
+    float ka[TILE * pitch(K)], va[TILE * pitch(K)];
+};
+// place of a token's plane: spread so that neither access pattern below meets a bank twice
+template <int K> __device__ __forceinline__ int place(int token, int plane)
+{
+    if (pitch(K) == 4) return token * 4 + (plane ^ (token >> 1 & 3));
+    if (pitch(K) == 2) return token * 2 + (plane ^ (token >> 2 & 1));
+    return token;
+}
+
+template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from, bool real)
+{
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+    const int n = real ? BYTES : 0;                 // (nothing is read for the others: zeros are written)
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(from), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" :: "r"(dst), "l"(from), "r"(n), "n"(BYTES) : "memory");
+}
+
+__device__ __forceinline__ void mma_s8u8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+
+// The products run on the integer tensor cores, on the planes' bits as they are stored: a word ANDed with 0x01010101 << j is four bytes of 0 or
+// 2^j, an operand of mma.m16n8k32 with the query (or the weights) as digits of eight bits.  A query row is four rows of the operand, its
+// digits, so that four query rows fill the 16 rows of an instruction, and the product is exact:
+//   q = sum_digits 256^i d_i (31-bit fixed point; elements whose bits lie at position j of a byte are held divided by 2^j),
+//   q . b = 2 sum_{bit = 1} q - sum q.
+// Nothing else in this kernel is near the tensor cores' or the memory's pace: per 8 tokens of 4 bits 64 AND, 33 MMAs, 1280 bytes.
+//
+// A warp takes tiles of 32 tokens on its own (its copies, through a ring of its own stages; the softmax's running maximum and sum; partial sums), the
+// CTA's four warps are joined at the end, and shares of a sequence (`splits`) by a second kernel.
+//
+// Lane l = 4 g + c of an MMA holds rows g and g + 8: digits g / 4 and 2 + g / 4 of query row g mod 4.  For keys, column g is token g of eight and c the
+// word of the plane; results are those of tokens 2 c, 2 c + 1.  For values, c stands for the same two tokens, so weights never change
+// lanes, and column g for dimensions 16 g .. 16 g + 15, one per MMA.
+template <int K>
+__global__ void __launch_bounds__(WARPS * 32, 3)
 cache_attention_kernel(const __grid_constant__ AttentionParams p)
 {
-    __shared__ float s_m[4], s_l[4], s_o[4][AMQ_MAX_HEAD_DIM];
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
+    const CacheView& cv = p.c;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3, r = g & 3;
+    const bool upper = g < 4;           // rows g, g + 8: digits 3 and 1 of the query (weights: 2 and 0), else 2 and 0 (1 and none)
+    Stage<K>* stages = reinterpret_cast<Stage<K>*>(smem_raw) + warp * STAGES;
+
+    int at = blockIdx.x;
+    const int rb = at % p.row_blocks; at /= p.row_blocks;
+    const int kv = at % cv.heads; at /= cv.heads;
+    const int split = at % p.splits, b = at / p.splits;
+
     grid_dependency_wait();
-    const CacheView& c = p.c;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int h = blockIdx.x % p.q_heads, i = blockIdx.x / p.q_heads % p.q_len, b = blockIdx.x / p.q_heads / p.q_len, kv = h / p.group;
-    const int seen = visible_length(c, b) - p.q_len + 1 + i;
-    const float* q = p.q + b * p.q_batch + i * p.q_token + h * p.q_head;
-    float qv[DPL], o[DPL];
+    const int length = visible_length(cv, b);
+    const int last_row = min(rb * ROWS + ROWS, p.rows) - 1;
+    const int limit = max(length - p.q_len + 1 + last_row / p.group, 0);        // of the block's last row: no other sees more
+    const int row = rb * ROWS + r;
+    const int my_limit = row < p.rows ? length - p.q_len + 1 + row / p.group : 0;
+    const int tiles = limit > 0 ? (limit - 1) / TILE + 1 : 0;
+    const int tile0 = (int)((long long)tiles * split / p.splits), tile1 = (int)((long long)tiles * (split + 1) / p.splits);
+
+    auto slot_at = [&](int tile) {
+        const int t = tile * TILE + lane;
+        return tile < tile1 && t < limit ? slot_of(cv, b, t) : -1ll;
+    };
+    auto issue = [&](Stage<K>& st, long long slot) {
+        const uint4* kc = reinterpret_cast<const uint4*>(cv.kcodes) + (size_t)kv * K;
+        const uint4* vc = reinterpret_cast<const uint4*>(cv.vcodes) + (size_t)kv * K;
+        const size_t step = (size_t)cv.heads * K;
 #pragma unroll
-    for (int j = 0; j < DPL; ++j) { qv[j] = lane + 32 * j < c.d ? q[lane + 32 * j] : 0.0f; o[j] = 0.0f; }
-    float m = -INFINITY, l = 0.0f;
-    for (int t = warp; t < seen; t += 4) {
-        const long long slot = slot_of(c, b, t);
-        if (slot < 0) continue;
-        const size_t row = ((size_t)slot * c.heads + kv) * c.k;
-        float s = 0.0f;
-        for (int pl = 0; pl < c.k; ++pl) {
-            float dot = 0.0f;
+        for (int i = 0; i < K; ++i) {
+            const int idx = i * 32 + lane, token = idx / K, plane = idx % K;
+            const long long s = __shfl_sync(0xffffffffu, slot, token);
+            const size_t from = s < 0 ? 0 : (size_t)s * step + plane;
+            copy_async<16>(&st.k[place<K>(token, plane)], kc + from, s >= 0);
+            copy_async<16>(&st.v[place<K>(token, plane)], vc + from, s >= 0);
+        }
+        const size_t from = (slot < 0 ? 0 : (size_t)slot * step) + (size_t)kv * K;
+        float *ka = st.ka + lane * pitch(K), *va = st.va + lane * pitch(K);
+        constexpr int UNIT = K == 3 ? 1 : K;
+        if (p.wide) {
 #pragma unroll
-            for (int j = 0; j < DPL; ++j) dot += (c.kcodes[(row + pl) * c.wpr + j] >> lane & 1) ? qv[j] : -qv[j];
-            s += c.kcoeffs[row + pl] * dot;
+            for (int i = 0; i < K; i += UNIT) {
+                copy_async<4 * UNIT>(ka + i, cv.kcoeffs + from + i, slot >= 0);
+                copy_async<4 * UNIT>(va + i, cv.vcoeffs + from + i, slot >= 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                copy_async<4>(ka + i, cv.kcoeffs + from + i, slot >= 0);
+                copy_async<4>(va + i, cv.vcoeffs + from + i, slot >= 0);
+            }
+        }
+    };
+    auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+
+    int tile = tile0 + warp;
+    uint32_t real[STAGES];              // tokens on a page, per stage
+    long long slot = slot_at(tile);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        const long long now = slot;
+        slot = slot_at(tile + (s + 1) * WARPS);
+        real[s] = __ballot_sync(0xffffffffu, now >= 0);
+        if (real[s]) issue(stages[s], now);
+        commit();
+    }
+
+    // the query's digits as the MMAs take them, and the digits' sums (times the bytes' weights) over the row
+    uint32_t aq[4][4];
+    float half_sum[2], factor;
+    {
+        float x[32];
+        uint32_t largest = 0;
+        const int i = row / p.group, h = kv * p.group + row % p.group;
+        const float* q = p.q + b * p.q_batch + i * p.q_token + h * p.q_head + 32 * c;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            x[j] = row < p.rows && 32 * c + j < cv.d ? q[j] : 0.0f;
+            largest = max(largest, __float_as_uint(x[j]) & 0x7fffffffu);
+        }
+        largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
+        largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
+        const int e = max((int)(largest >> 23), 29);
+        const bool finite = largest < 0x7f800000u;
+        const float to_fixed = finite ? __int_as_float((283 - e) << 23) : 0.0f;         // largest element below 2^30
+        int sum[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t a0 = 0, a1 = 0;
+#pragma unroll
+            for (int byte = 0; byte < 4; ++byte) {
+                const uint32_t y = (uint32_t)__float2int_rn(x[j + 8 * byte] * to_fixed * (1.0f / (1 << j))) + 0x80808080u;
+                const int d0 = (int)((upper ? y >> 24 : y >> 16) & 255u) - 128, d1 = (int)((upper ? y >> 8 : y) & 255u) - 128;
+                a0 |= (uint32_t)(d0 & 255) << (8 * byte);
+                a1 |= (uint32_t)(d1 & 255) << (8 * byte);
+                sum[0] += d0 * (1 << j); sum[1] += d1 * (1 << j);
+            }
+            aq[j >> 1][(j & 1) * 2] = a0;
+            aq[j >> 1][(j & 1) * 2 + 1] = a1;
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        s *= p.scale;
-        const float m_new = fmaxf(m, s), corr = expf(m - m_new), w = expf(s - m_new);
-        l = l * corr + w;
-#pragma unroll
-        for (int j = 0; j < DPL; ++j) o[j] *= corr;
-        for (int pl = 0; pl < c.k; ++pl) {
-            const float a = w * c.vcoeffs[row + pl];
-#pragma unroll
-            for (int j = 0; j < DPL; ++j) o[j] += (c.vcodes[(row + pl) * c.wpr + j] >> lane & 1) ? a : -a;
+        for (int w = 0; w < 2; ++w) {
+            sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], 1);
+            sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], 2);
+            half_sum[w] = 0.5f * (float)sum[w];
         }
+        factor = finite ? 1.0f / to_fixed * p.scale * (2.0f * 1.44269504f) : NAN;       // scores in units of log 2
+    }
+    const float w0 = upper ? 16777216.0f : 65536.0f, w1 = upper ? 256.0f : 1.0f;        // digits' weights: keys
+    const float wv = upper ? 65536.0f : 256.0f;                                         // values (row g + 8: 1 or nothing)
+    const uint32_t sel = upper ? 0x62u : 0x51u, keep = upper ? 0xffffffffu : 0u;
+    const uint32_t half = g & 1 ? 0x7362u : 0x5140u;        // bytes of the plane words that hold dimensions 16 g ..
+
+    float m = -INFINITY, l = 0.0f, o[16][2];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j][0] = o[j][1] = 0.0f;
+
+    int stage = 0;
+    for (; tile < tile1; tile += WARPS) {
+        {
+            const long long now = slot;
+            slot = slot_at(tile + STAGES * WARPS);
+            real[STAGES - 1] = __ballot_sync(0xffffffffu, now >= 0);
+            __syncwarp();
+            if (real[STAGES - 1]) issue(stages[stage == 0 ? STAGES - 1 : stage - 1], now);
+            commit();
+            asm volatile("cp.async.wait_group %0;" :: "n"(STAGES - 1) : "memory");
+            __syncwarp();
+        }
+        const Stage<K>& st = stages[stage];
+        const uint32_t on_a_page = real[0];
+#pragma unroll
+        for (int q = 0; q < STAGES - 1; ++q) real[q] = real[q + 1];
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        if (on_a_page == 0) continue;           // (nothing was copied)
+        // tokens that this lane's row sees, from token 2 c on
+        const int left = my_limit - tile * TILE;
+        const uint32_t mask = (on_a_page & (left >= TILE ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u)) >> (2 * c);
+
+        // scores of tokens 8 n + 2 c, 8 n + 2 c + 1
+        float s[4][2];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            int acc[K][4];
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = MAGIC_BITS;
+                const uint32_t w = reinterpret_cast<const uint32_t*>(&st.k[place<K>(8 * n + g, i)])[c];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_s8u8(acc[i], aq[j], w & (0x01010101u << (2 * j)), w & (0x02020202u << (2 * j)));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float* a = st.ka + (8 * n + 2 * c + e) * pitch(K);
+                float x = 0.0f, y = 0.0f, all = 0.0f;
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    x = fmaf(a[i], __int_as_float(acc[i][e]) - MAGIC, x);
+                    y = fmaf(a[i], __int_as_float(acc[i][2 + e]) - MAGIC, y);
+                    all += a[i];
+                }
+                x = fmaf(-half_sum[0], all, x);
+                y = fmaf(-half_sum[1], all, y);
+                float v = fmaf(w0, x, w1 * y);
+                v += __shfl_xor_sync(0xffffffffu, v, 16);
+                s[n][e] = mask >> (8 * n + e) & 1 ? v * factor : -INFINITY;
+            }
+        }
+        // weights, relative to the tile's maximum
+        float top = s[0][0];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(s[n][0], s[n][1]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const float ref = top == -INFINITY ? 0.0f : top, m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.0f : m_new;
+        const float corr = exp2_approx(m - m_ref), tile_factor = exp2_approx(top - m_ref);
         m = m_new;
-    }
-    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+        // the values' coefficients: the largest decides the fixed point
+        float va[4][2][K];
+        uint32_t largest = 0;
 #pragma unroll
-    for (int j = 0; j < DPL; ++j) s_o[warp][lane + 32 * j] = o[j];
-    __syncthreads();
-    const float M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    float total = 0.0f, sum = 0.0f;
-    for (int w = 0; w < 4; ++w) {
-        const float f = s_l[w] == 0.0f ? 0.0f : expf(s_m[w] - M);
-        total += s_l[w] * f;
-        sum += s_o[w][threadIdx.x] * f;
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    va[n][e][i] = st.va[(8 * n + 2 * c + e) * pitch(K) + i];
+                    largest = max(largest, __float_as_uint(va[n][e][i]) & 0x7fffffffu);
+                }
+        largest = __reduce_max_sync(0xffffffffu, largest);
+        if (largest >= 0x7f800000u) {           // NaN or infinite coefficients: nobody's but the rows' that see them
+            largest = 0;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        if (!isfinite(va[n][e][i])) {
+                            if (mask >> (8 * n + e) & 1) l = NAN;
+                            va[n][e][i] = 0.0f;
+                        }
+                        largest = max(largest, __float_as_uint(va[n][e][i]) & 0x7fffffffu);
+                    }
+            largest = __reduce_max_sync(0xffffffffu, largest);
+        }
+        const int ev = max((int)(largest >> 23), 22);
+        const float to_fixed = __int_as_float((275 - ev) << 23), from_fixed = __int_as_float((ev - 21) << 23);
+        float sum = 0.0f;
+        // weights times coefficients as digits: an MMA's 32 positions are 32 / pitch tokens, 8 / pitch of them this lane's
+        constexpr int PK = pitch(K), STEPS = PK, PER = 4 / PK;          // MMA steps of a tile; tokens in a register of four bytes
+        uint32_t ap[STEPS][4], bv[STEPS][2][2];
+#pragma unroll
+        for (int z = 0; z < STEPS; ++z)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                uint32_t y[4], word[4];
+#pragma unroll
+                for (int u = 0; u < PER; ++u) {
+                    // this lane's tokens in order: (n, e) = (0, 0), (0, 1), (1, 0), ..
+                    const int q = (2 * z + side) * PER + u, n = q >> 1, e = q & 1;
+                    const float w = exp2_approx(s[n][e] - ref);
+                    sum += w;
+                    const float ws = w * to_fixed;
+#pragma unroll
+                    for (int i = 0; i < PK; ++i) {
+                        y[u * PK + i] = i < K ? (uint32_t)__float_as_int(fmaf(ws, va[n][e][i < K ? i : 0], MAGIC)) + (0x00808080u - (uint32_t)MAGIC_BITS) : 0x00808080u;
+                        word[u * PK + i] = i < K ? reinterpret_cast<const uint32_t*>(&st.v[place<K>(8 * n + 2 * c + e, i < K ? i : 0)])[g >> 1] : 0u;
+                    }
+                }
+                ap[z][2 * side] = __byte_perm(__byte_perm(y[0], y[1], sel), __byte_perm(y[2], y[3], sel), 0x5410) ^ 0x80808080u;
+                ap[z][2 * side + 1] = (__byte_perm(__byte_perm(y[0], y[1], 0x40), __byte_perm(y[2], y[3], 0x40), 0x5410) ^ 0x80808080u) & keep;
+                const uint32_t t0 = __byte_perm(word[0], word[1], half), t1 = __byte_perm(word[2], word[3], half);
+                bv[z][side][0] = __byte_perm(t0, t1, 0x5410);
+                bv[z][side][1] = __byte_perm(t0, t1, 0x7632);
+            }
+        l = fmaf(l, corr, sum * tile_factor);
+        int ones[4] = {MAGIC_BITS, MAGIC_BITS, MAGIC_BITS, MAGIC_BITS};
+#pragma unroll
+        for (int z = 0; z < STEPS; ++z) mma_s8u8(ones, ap[z], 0x01010101u, 0x01010101u);
+        const float unit = tile_factor * from_fixed;
+        const float base = -unit * fmaf(wv, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            int acc[4] = {MAGIC_BITS, MAGIC_BITS, MAGIC_BITS, MAGIC_BITS};
+#pragma unroll
+            for (int z = 0; z < STEPS; ++z) mma_s8u8(acc, ap[z], bv[z][0][j >> 3] & (0x01010101u << (j & 7)), bv[z][1][j >> 3] & (0x01010101u << (j & 7)));
+            const float f = unit * (2.0f / (1 << (j & 7)));
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                o[j][e] = fmaf(fmaf(wv, __int_as_float(acc[e]) - MAGIC, __int_as_float(acc[2 + e]) - MAGIC), f, fmaf(o[j][e], corr, base));
+        }
     }
-    if (threadIdx.x < c.d) p.out[(size_t)blockIdx.x * c.d + threadIdx.x] = total == 0.0f ? 0.0f : sum / total;
+
+    // this warp's tokens together: sums over the lanes of a row, then over the warps through shared memory (the stages' memory, once the copies are done)
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    float (*s_o)[ROWS][AMQ_MAX_HEAD_DIM] = reinterpret_cast<float (*)[ROWS][AMQ_MAX_HEAD_DIM]>(smem_raw);
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float v = o[j][e] + __shfl_xor_sync(0xffffffffu, o[j][e], 16);
+            if (upper) s_o[warp][r][32 * c + 16 * e + j] = v;
+        }
+    if (lane < 16 && c == 0) { s_m[warp][r] = m; s_l[warp][r] = l; }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+        const int rho = rb * ROWS + q;
+        if (rho >= p.rows) break;
+        const float M = fmaxf(fmaxf(s_m[0][q], s_m[1][q]), fmaxf(s_m[2][q], s_m[3][q])), m_ref = M == -INFINITY ? 0.0f : M;
+        float total = 0.0f, v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = exp2_approx(s_m[w][q] - m_ref);
+            total += s_l[w][q] * f;
+            v += s_o[w][q][threadIdx.x] * f;
+        }
+        const size_t orow = ((size_t)b * p.q_len + rho / p.group) * p.q_heads + kv * p.group + rho % p.group;
+        if (p.splits == 1) {
+            if ((int)threadIdx.x < cv.d) p.out[orow * cv.d + threadIdx.x] = total == 0.0f ? 0.0f : v / total;
+        } else {
+            p.part[(orow * p.splits + split) * AMQ_MAX_HEAD_DIM + threadIdx.x] = v;
+            if (threadIdx.x == 0) p.part_ml[orow * p.splits + split] = make_float2(M, total);
+        }
+    }
+}
+
+// joins the shares of a query row: one CTA per row
+__global__ void __launch_bounds__(AMQ_MAX_HEAD_DIM)
+cache_attention_join_kernel(const float* part, const float2* part_ml, int splits, int d, float* out)
+{
+    grid_dependency_wait();
+    const size_t row = blockIdx.x;
+    float M = -INFINITY;
+    for (int s = 0; s < splits; ++s) M = fmaxf(M, __ldcg(part_ml + row * splits + s).x);
+    const float m_ref = M == -INFINITY ? 0.0f : M;
+    float total = 0.0f, v = 0.0f;
+    for (int s = 0; s < splits; ++s) {
+        const float2 ml = __ldcg(part_ml + row * splits + s);
+        const float f = exp2_approx(ml.x - m_ref);
+        total += ml.y * f;
+        v += __ldcg(part + (row * splits + s) * AMQ_MAX_HEAD_DIM + threadIdx.x) * f;
+    }
+    if ((int)threadIdx.x < d) out[row * d + threadIdx.x] = total == 0.0f ? 0.0f : v / total;
+}
+
+struct AttentionPlan { int rows, row_blocks, splits; size_t part_bytes, bytes; };
+
+AttentionPlan attention_plan(int batch, int q_len, int q_heads, int heads, long long max_tokens)
+{
+    AttentionPlan a{};
+    a.rows = q_len * (q_heads / heads);
+    a.row_blocks = (a.rows + ROWS - 1) / ROWS;
+    const long long base = (long long)batch * heads * a.row_blocks;
+    long long splits = (1184 + base - 1) / base;
+    const long long most = (max_tokens + 511) / 512;
+    if (splits > most) splits = most;
+    if (splits > 128) splits = 128;
+    a.splits = splits < 1 ? 1 : (int)splits;
+    if (a.splits > 1) {
+        const size_t n = (size_t)batch * q_len * q_heads * a.splits;
+        a.part_bytes = n * AMQ_MAX_HEAD_DIM * 4;
+        a.bytes = a.part_bytes + n * sizeof(float2);
+    }
+    return a;
+}
+
+template <int K>
+amq_status launch_attention(const AttentionParams& p, unsigned grid, cudaStream_t st)
+{
+    const size_t smem = sizeof(Stage<K>) * STAGES * WARPS > sizeof(float) * WARPS * ROWS * AMQ_MAX_HEAD_DIM ? sizeof(Stage<K>) * STAGES * WARPS
+                                                                                                       : sizeof(float) * WARPS * ROWS * AMQ_MAX_HEAD_DIM;
+    AMQ_CUDA_TRY(cudaFuncSetAttribute(cache_attention_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    AMQ_CUDA_TRY(launch_kernel(cache_attention_kernel<K>, dim3(grid), dim3(WARPS * 32), smem, st, true, p));
+    AMQ_LAUNCH_CHECK();
+    return AMQ_OK;
 }
 
 amq_status cache_view(const uint32_t* kcodes, const float* kcoeffs, const uint32_t* vcodes, const float* vcoeffs, int pages, int page_size, int heads,
@@ -126,7 +471,7 @@ amq_status cache_view(const uint32_t* kcodes, const float* kcoeffs, const uint32
 {
     if (pages < 0 || page_size < 1 || heads < 1 || d < 1 || max_pages < 0 || ld_table < max_pages) return AMQ_ERR_INVALID_ARG;
     if (!valid_k(k) || d > AMQ_MAX_HEAD_DIM || heads > 65535) return AMQ_ERR_UNSUPPORTED;
-    if ((long long)max_pages * page_size > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
+    if ((long long)max_pages * page_size > AMQ_MAX_TOKENS) return AMQ_ERR_UNSUPPORTED;
     *out = {kcodes, kcoeffs, vcodes, vcoeffs, pages, page_size, heads, d, k, words_per_row(d), table, ld_table, max_pages, lengths};
     return AMQ_OK;
 }
@@ -162,7 +507,8 @@ amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs, const 
 
 size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens)
 {
-    return 0;
+    if (batch < 1 || q_len < 1 || q_heads < 1 || heads < 1 || q_heads % heads || d < 1 || d > AMQ_MAX_HEAD_DIM || max_tokens < 1) return 0;
+    return amq::attention_plan(batch, q_len, q_heads, heads, max_tokens).bytes;
 }
 
 amq_status amq_cache_attention(const float* q, long long q_batch, long long q_token, long long q_head,
@@ -172,8 +518,8 @@ amq_status amq_cache_attention(const float* q, long long q_batch, long long q_to
                                void* workspace, size_t workspace_bytes, void* stream)
 {
     amq::AttentionParams p{};
-    const amq_status s = amq::cache_view(cache_kcodes, cache_kcoeffs, cache_vcodes, cache_vcoeffs, pages, page_size, heads, d, k, table, ld_table, max_pages,
-                                         lengths, &p.c);
+    amq_status s = amq::cache_view(cache_kcodes, cache_kcoeffs, cache_vcodes, cache_vcoeffs, pages, page_size, heads, d, k, table, ld_table, max_pages,
+                                   lengths, &p.c);
     if (s != AMQ_OK) return s;
     if (batch < 0 || q_len < 0 || q_heads < 1 || q_heads % heads) return AMQ_ERR_INVALID_ARG;
     if ((long long)batch * q_len * q_heads > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
@@ -181,9 +527,29 @@ amq_status amq_cache_attention(const float* q, long long q_batch, long long q_to
     if (!q || !out || !lengths || (max_pages > 0 && !table)) return AMQ_ERR_INVALID_ARG;
     if (pages > 0 && (!cache_kcodes || !cache_kcoeffs || !cache_vcodes || !cache_vcoeffs)) return AMQ_ERR_INVALID_ARG;
     if (!amq::aligned16(cache_kcodes) || !amq::aligned16(cache_vcodes)) return AMQ_ERR_ALIGNMENT;
+    const amq::AttentionPlan plan = amq::attention_plan(batch, q_len, q_heads, heads, (long long)max_pages * page_size);
+    const long long grid = (long long)batch * heads * plan.row_blocks * plan.splits;
+    if (grid > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
+    if (plan.bytes) {
+        if (!workspace || workspace_bytes < plan.bytes) return AMQ_ERR_WORKSPACE;
+        if (!amq::aligned16(workspace)) return AMQ_ERR_ALIGNMENT;
+    }
     p.q = q; p.q_batch = q_batch; p.q_token = q_token; p.q_head = q_head;
     p.q_len = q_len; p.q_heads = q_heads; p.group = q_heads / heads; p.scale = scale; p.out = out;
-    AMQ_CUDA_TRY(amq::launch_kernel(amq::cache_attention_kernel, dim3((unsigned)(batch * q_len * q_heads)), dim3(128), 0, (cudaStream_t)stream, true, p));
+    p.rows = plan.rows; p.row_blocks = plan.row_blocks; p.splits = plan.splits;
+    p.part = static_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.part_bytes);
+    p.wide = amq::aligned16(cache_kcoeffs) && amq::aligned16(cache_vcoeffs);
+    cudaStream_t st = (cudaStream_t)stream;
+    switch (k) {
+        case 1: s = amq::launch_attention<1>(p, (unsigned)grid, st); break;
+        case 2: s = amq::launch_attention<2>(p, (unsigned)grid, st); break;
+        case 3: s = amq::launch_attention<3>(p, (unsigned)grid, st); break;
+        default: s = amq::launch_attention<4>(p, (unsigned)grid, st); break;
+    }
+    if (s != AMQ_OK || plan.splits == 1) return s;
+    AMQ_CUDA_TRY(amq::launch_kernel(amq::cache_attention_join_kernel, dim3((unsigned)(batch * q_len * q_heads)), dim3(AMQ_MAX_HEAD_DIM), 0, st, true, p.part, p.part_ml,
+                                    plan.splits, d, out));
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;
 }
