@@ -189,30 +189,16 @@ def binary_gemm(Wcodes, Walpha, xcodes, xbeta, n, bias=None, y=None):
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, ACT_TANH, ACT_SIGMOID = range(6)
 
 
-def _rows(t, name, rows, cols):
-    """Leading dimension of a 2-D CUDA fp32 tensor of that shape with contiguous rows (any row stride)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.float32 and tuple(t.shape) == (rows, cols)
-            and (cols == 1 or t.stride(1) == 1)):
-        raise TypeError("%s must be a CUDA float32 tensor of shape (%d, %d) with contiguous rows" % (name, rows, cols))
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
-
-
-def _shaped(t, name, *shape):
-    """Raises unless t is None or a tensor of that shape (its type, device and strides are looked at where its address is taken)."""
-    if t is not None and tuple(t.shape) != shape:
-        raise TypeError("%s must have the shape %s" % (name, shape))
+def _result(r):
+    """What a native call answers: its results, or the status of a call that the library refused."""
+    if r.__class__ is int:
+        _check(r)
+    return r
 
 
 def binary_gemm_act(Wcodes, Walpha, xcodes, xbeta, n, bias=None, activation=ACT_NONE, residual=None, y=None):
     """binary_gemm with an activation and a residual (batch, m) behind it -> y (batch, m) fp32; y may be the residual."""
-    m, k_w, _ = Wcodes.shape
-    batch, k_a, _ = xcodes.shape
-    if y is None:
-        y = _native.empty(Wcodes, 0, batch, m)
-    ldr = 0 if residual is None else _rows(residual, "residual", batch, m)
-    _check(_native.amq_binary_gemm_act(Wcodes, Walpha, m, n, k_w, xcodes, xbeta, batch, k_a, bias, activation,
-                                       None if residual is None else residual.data_ptr(), ldr, y.data_ptr(), _rows(y, "y", batch, m)))
-    return y
+    return _result(_native.binary_gemm_act(Wcodes, Walpha, xcodes, xbeta, n, bias, activation, residual, y))
 
 
 def quantized_gemv(Wcodes, Walpha, x, k_a, T, bias=None, y=None, want_codes=False):
@@ -455,28 +441,9 @@ def new_cache(pages, page_size, heads, d, k, device="cuda"):
                  for shape, dtype in ((codes, torch.int32), (coeffs, torch.float32), (codes, torch.int32), (coeffs, torch.float32)))
 
 
-def _cache(cache, table, lengths, d):
-    """(pages, page_size, heads, d, k, table, ld_table, max_pages), the shapes checked against one another."""
-    kcodes, kcoeffs, vcodes, vcoeffs = cache
-    pages, page_size, heads, k, wpr = kcodes.shape
-    if wpr != 4 * ((d + 127) // 128) or vcodes.shape != kcodes.shape or kcoeffs.shape != kcodes.shape[:4] or vcoeffs.shape != kcoeffs.shape:
-        raise TypeError("a cache is (kcodes, kcoeffs, vcodes, vcoeffs) of shapes (pages, page_size, heads, k[, words of a plane])")
-    if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and (table.shape[1] <= 1 or table.stride(1) == 1)
-            and lengths.shape == table.shape[:1]):
-        raise TypeError("table must be a CUDA int32 tensor (batch, pages of a sequence) with contiguous rows, lengths (batch,)")
-    batch, max_pages = table.shape
-    return pages, page_size, heads, d, k, table.data_ptr(), table.stride(0) if batch > 1 else max(max_pages, table.stride(0)), max_pages
-
-
 def cache_append(kcodes, kcoeffs, vcodes, vcoeffs, cache, table, lengths, d):
     """Quantized rows (batch, count, heads, k[, words]) of every sequence's newest tokens -> their places in the cache (see amq.h)."""
-    view = _cache(cache, table, lengths, d)
-    batch, count = kcodes.shape[:2]
-    _shaped(kcodes, "kcodes", table.shape[0], count, view[2], view[4], cache[0].shape[4])
-    _shaped(vcodes, "vcodes", *kcodes.shape)
-    _shaped(kcoeffs, "kcoeffs", *kcodes.shape[:4])
-    _shaped(vcoeffs, "vcoeffs", *kcodes.shape[:4])
-    _check(_native.amq_cache_append(kcodes, kcoeffs, vcodes, vcoeffs, *cache, *view, lengths, batch, count))
+    _check(_native.cache_append(kcodes, kcoeffs, vcodes, vcoeffs, cache, table, lengths, d))
 
 
 def cache_attention_workspace_bytes(batch, q_len, q_heads, heads, d, max_tokens):
@@ -490,20 +457,7 @@ def new_cache_attention_workspace(batch, q_len, q_heads, heads, d, max_tokens, d
 def cache_attention(q, cache, table, lengths, scale, workspace=None, out=None):
     """q (batch, q_len, q_heads, d) fp32, any strides but the last, of every sequence's newest tokens -> out, contiguous, of q's shape.
     Without a workspace one is taken from PyTorch's allocator for the call."""
-    if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dtype == torch.float32 and q.dim() == 4 and (q.shape[3] == 1 or q.stride(3) == 1)):
-        raise TypeError("q must be a CUDA float32 tensor (batch, q_len, q_heads, d) with contiguous rows")
-    batch, q_len, q_heads, d = q.shape
-    view = _cache(cache, table, lengths, d)
-    if table.shape[0] != batch:
-        raise TypeError("q and table must agree in their first dimension")
-    if workspace is None:
-        workspace = new_cache_attention_workspace(batch, q_len, q_heads, view[2], d, view[7] * view[1], q.device)
-    if out is None:
-        out = _native.empty(q, 0, batch, q_len, q_heads, d)
-    _shaped(out, "out", batch, q_len, q_heads, d)
-    _check(_native.amq_cache_attention(q.data_ptr(), q.stride(0), q.stride(1), q.stride(2), *cache, *view, lengths, batch, q_len, q_heads, scale,
-                                       out, workspace, workspace.numel()))
-    return out
+    return _result(_native.cache_attention(q, cache, table, lengths, scale, workspace, out))
 
 
 MAX_BEAMS = 32
@@ -513,13 +467,7 @@ MAX_STATES = 8
 def beam_select(logits, scores, finished=None, eos=-1):
     """logits (batch * beams, vocab) fp32, rows contiguous (any row stride); scores (batch, beams) fp32; finished (batch, beams) int32 or None
     -> (scores fp32, parents int32, tokens int32, finished int32), all (batch, beams), best first."""
-    batch, beams = scores.shape
-    ld = _rows(logits, "logits", batch * beams, logits.shape[-1])
-    _shaped(finished, "finished", batch, beams)
-    best = _native.empty(scores, 0, batch, beams)
-    parents, tokens, ended = (_native.empty(scores, 1, batch, beams) for _ in range(3))
-    _check(_native.amq_beam_select(logits.data_ptr(), ld, logits.shape[1], scores, finished, eos, batch, beams, best, parents, tokens, ended))
-    return best, parents, tokens, ended
+    return _result(_native.beam_select(logits, scores, finished, eos))
 
 
 def beam_reorder(states, parents, out=None):

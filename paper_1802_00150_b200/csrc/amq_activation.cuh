@@ -2,22 +2,46 @@
 // that a product alone keeps the registers and instructions that it had.
 #pragma once
 
+#include <type_traits>
+
 #include "amq_common.cuh"
 
 namespace amq {
 
-// erfcf, expf and tanhf rather than the fast forms: an activation is a few instructions of a thread that has just folded hundreds of
-// products, and its result is then as near to the exact one as the product is.
+// erfcf, expf and tanhf rather than the fast forms: an activation is a few instructions of a thread that has just folded dozens of integers, and its
+// result is then as near to the exact one as the product is.
+template <int ACTIVATION> __device__ __forceinline__ float activate(float v)
+{
+    if (ACTIVATION == AMQ_ACT_RELU) return v < 0.0f ? 0.0f : v;                      // (NaN stays NaN)
+    if (ACTIVATION == AMQ_ACT_GELU) return 0.5f * v * erfcf(-0.70710678f * v);       // v Phi(v); through erfc, so that nothing cancels for v << 0
+    if (ACTIVATION == AMQ_ACT_SILU) return __fdividef(v, 1.0f + expf(-v));           // (a denominator beyond 2^126 gives 0, the result's limit)
+    if (ACTIVATION == AMQ_ACT_TANH) return tanhf(v);
+    if (ACTIVATION == AMQ_ACT_SIGMOID) return __fdividef(1.0f, 1.0f + expf(-v));
+    return v;
+}
+
+// N values at once: one choice for all of them
+template <int N> __device__ __forceinline__ void activate(float (&v)[N], int activation)
+{
+    auto all = [&](auto kind) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = activate<decltype(kind)::value>(v[i]);
+    };
+    switch (activation) {
+        case AMQ_ACT_RELU: all(std::integral_constant<int, AMQ_ACT_RELU>{}); break;
+        case AMQ_ACT_GELU: all(std::integral_constant<int, AMQ_ACT_GELU>{}); break;
+        case AMQ_ACT_SILU: all(std::integral_constant<int, AMQ_ACT_SILU>{}); break;
+        case AMQ_ACT_TANH: all(std::integral_constant<int, AMQ_ACT_TANH>{}); break;
+        case AMQ_ACT_SIGMOID: all(std::integral_constant<int, AMQ_ACT_SIGMOID>{}); break;
+        default: break;
+    }
+}
+
 __device__ __forceinline__ float activate(float v, int activation)
 {
-    switch (activation) {
-        case AMQ_ACT_RELU: return v < 0.0f ? 0.0f : v;                       // (NaN stays NaN)
-        case AMQ_ACT_GELU: return 0.5f * v * erfcf(-0.70710678f * v);        // v Phi(v); through erfc, so that nothing cancels for v << 0
-        case AMQ_ACT_SILU: return v / (1.0f + expf(-v));
-        case AMQ_ACT_TANH: return tanhf(v);
-        case AMQ_ACT_SIGMOID: return 1.0f / (1.0f + expf(-v));
-        default: return v;
-    }
+    float a[1] = {v};
+    activate(a, activation);
+    return a[0];
 }
 
 }  // namespace amq

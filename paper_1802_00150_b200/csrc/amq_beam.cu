@@ -7,10 +7,11 @@
 // than fp32 rounding of a score of -20 (2e-6), those of one beam never change places.
 //
 // A cluster of eight CTAs takes a batch entry; CTA c reads the eighth c of every beam's row, so any number of beams is balanced, and one entry
-// alone still has eight SMs.  A group of 256 threads holds a beam's eighth in registers (in pieces where it has more than 6144 words), one word a
-// lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's sum does not depend
-// on where it starts: equal rows get equal sums.  The K-th largest of the maxima of 32 groups of eight lanes is a lower bound of the eighth's K-th
-// largest logit, and little more than K logits reach it; those are written down.
+// alone still has eight SMs.  A group of 256 threads takes a beam's eighth in pieces of up to twelve words a thread, the next piece on its way while
+// one is worked on: one word a lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's
+// sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the eighth's K-th largest logit comes from the maxima of 32 groups of
+// eight threads, and little more than K logits reach it; those are written down, sorted by counting, and go to the first CTA's shared memory, which
+// joins the eight by score.
 #include <cooperative_groups.h>
 
 #include "amq_common.cuh"
@@ -21,9 +22,8 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int SLICES = 8;               // CTAs of a cluster
-constexpr int THREADS = 256;            // of a group; a CTA has one to four, each with beams of its own
-constexpr int WARPS = THREADS / 32;
-constexpr int MAX_GROUPS = 4;
+constexpr int MAX_THREADS = 1024;       // of a CTA: groups of 128 or 256 threads, each with beams of its own
+constexpr int MAX_GROUPS = 8, MAX_WARPS = 8;        // groups, warps of a group
 constexpr int CAP = 128;                // candidates kept of a beam's slice; where more pass the bound (ties), the slice is searched again
 
 struct SelectParams {
@@ -43,17 +43,19 @@ __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_flo
 // logits larger first, then tokens smaller first: one descending integer order
 __device__ __forceinline__ unsigned long long candidate(float v, int token) { return ((unsigned long long)ordered(v) << 32) | (uint32_t)~token; }
 
-struct WarpSum { float m, s; };         // largest logit and sum of exp(z - m) over a warp's share
+__device__ __forceinline__ float exp2_ftz(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+constexpr float LOG2E = 1.44269504f;
 
-// shared memory of a CTA: [beams][WARPS] sums, [beams][beams] sorted candidates, then working space
+// Sums of exp(z) as s 2^m, m = the largest logit times LOG2E, rounded: the exponents z LOG2E - m are one rounding each, and m / LOG2E in double takes
+// the roundings of m and of the constant back (what is left of them is 1e-8 (z - max)).
+struct WarpSum { float m, s; };
+
+// shared memory of a CTA.  What the others send lies in the first CTA's.
 struct SelectSmem {
-    WarpSum* sums;
-    unsigned long long* best;           // [beams][beams], 0 where there are fewer
+    WarpSum* sums;                      // [beams][SLICES][warps of a group], from every CTA
+    unsigned long long* best;           // [beams][SLICES][beams], from every CTA: sorted candidates, 0 where there are fewer
     unsigned long long* list;           // [beams][CAP] as found
     int* count;                         // [beams]
-    // rank 0: all candidates by score
-    double* total;                      // [SLICES * beams * beams]
-    int* pair;
 };
 
 __host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* base)
@@ -61,37 +63,78 @@ __host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* ba
     char* p = static_cast<char*>(base);
     size_t off = 0;
     auto take = [&](size_t bytes) { char* at = p + off; off += (bytes + 15) / 16 * 16; return at; };
-    char* sums = take(sizeof(WarpSum) * WARPS * beams);
-    char* best = take(8ull * beams * beams);
-    char* total = take(8ull * SLICES * beams * beams);      // (the lists are read before the scores are written)
-    char* pair = take(4ull * SLICES * beams * beams);
+    char* sums = take(sizeof(WarpSum) * SLICES * MAX_WARPS * beams);
+    char* best = take(8ull * SLICES * beams * beams);
     char* list = take(8ull * CAP * beams);
     char* count = take(4ull * beams);
     if (s) {
         s->sums = reinterpret_cast<WarpSum*>(sums); s->best = reinterpret_cast<unsigned long long*>(best);
-        s->list = reinterpret_cast<unsigned long long*>(list);
-        s->count = reinterpret_cast<int*>(count); s->total = reinterpret_cast<double*>(total); s->pair = reinterpret_cast<int*>(pair);
+        s->list = reinterpret_cast<unsigned long long*>(list); s->count = reinterpret_cast<int*>(count);
     }
     return off;
 }
 
 __device__ __forceinline__ uint32_t redux_max(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 
-// (score, pair) a before b
-__device__ __forceinline__ bool before(double a, int ai, double b, int bi) { return a > b || (a == b && ai < bi); }
+// doubles in the order of unsigned integers (finite ones)
+__device__ __forceinline__ unsigned long long ordered(double v)
+{
+    const unsigned long long u = (unsigned long long)__double_as_longlong(v);
+    return u ^ ((unsigned long long)((long long)u >> 63) | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double from_ordered(unsigned long long o)
+{
+    return __longlong_as_double((long long)(o ^ ((o >> 63) ? 0x8000000000000000ull : 0xffffffffffffffffull)));
+}
 
-// PT: words of a thread and piece
-template <int PT>
-__global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(THREADS * MAX_GROUPS)
+struct Choice { unsigned long long score; int pair; };       // score 0: none
+
+// One warp joins the sorted lists (one for each beam and slice): LISTS of them a lane, and beam after beam of the result the best of their heads,
+// by score, then pair.  `score_of(list, place)`.  Returns how many there were; lane 0 has written them down.
+template <int LISTS, typename F>
+__device__ __forceinline__ int join_lists(int K, F&& score_of, double* chosen, int* chosen_pair)
+{
+    const int lane = threadIdx.x & 31, lists = K * SLICES;
+    Choice head[LISTS];
+    int place[LISTS];
+#pragma unroll
+    for (int x = 0; x < LISTS; ++x) {
+        place[x] = 0;
+        head[x] = lane + 32 * x < lists ? score_of(lane + 32 * x, 0) : Choice{0ull, 0};
+    }
+    for (int r = 0; r < K; ++r) {
+        Choice best = head[0];
+        int from = 0;
+#pragma unroll
+        for (int x = 1; x < LISTS; ++x)
+            if (head[x].score > best.score || (head[x].score == best.score && head[x].pair < best.pair)) { best = head[x]; from = x; }
+        const uint32_t hi = redux_max((uint32_t)(best.score >> 32));
+        if (hi == 0u) return r;                     // (a finite score's high word is not 0)
+        const uint32_t lo = redux_max((uint32_t)(best.score >> 32) == hi ? (uint32_t)best.score : 0u);
+        const bool top = best.score == (((unsigned long long)hi << 32) | lo);
+        const uint32_t pair = __reduce_min_sync(0xffffffffu, top ? (uint32_t)best.pair : 0xffffffffu);
+        if (lane == 0) { chosen[r] = from_ordered(((unsigned long long)hi << 32) | lo); chosen_pair[r] = (int)pair; }
+        if (top && (uint32_t)best.pair == pair) {   // (pairs are distinct: one lane)
+#pragma unroll
+            for (int x = 0; x < LISTS; ++x)
+                if (x == from) head[x] = ++place[x] < K ? score_of(lane + 32 * x, place[x]) : Choice{0ull, 0};
+        }
+    }
+    return K;
+}
+
+// THREADS: of a group; PT: words of a thread and piece
+template <int THREADS, int PT>
+__global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(MAX_THREADS, 1)
 beam_select_kernel(SelectParams p)
 {
-    constexpr int CHUNK = THREADS * PT;
+    constexpr int CHUNK = THREADS * PT, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ float s_score[AMQ_MAX_BEAMS];
     __shared__ int s_done[AMQ_MAX_BEAMS];
     __shared__ double s_lse[AMQ_MAX_BEAMS];
     __shared__ uint32_t s_maxima[MAX_GROUPS][2][32];
-    __shared__ double s_cut; __shared__ int s_cut_pair; __shared__ int s_found;
+    __shared__ int s_found;
     __shared__ double s_chosen[AMQ_MAX_BEAMS]; __shared__ int s_chosen_pair[AMQ_MAX_BEAMS];
     cg::cluster_group cluster = cg::this_cluster();
     const int K = p.beams, tid = threadIdx.x, nthreads = blockDim.x, lane = tid & 31;
@@ -101,8 +144,24 @@ beam_select_kernel(SelectParams p)
     const int rank = (int)cluster.block_rank(), entry = blockIdx.x / SLICES;
     const int lo = (int)((long long)p.vocab * rank / SLICES), hi = (int)((long long)p.vocab * (rank + 1) / SLICES);
     const size_t row0 = (size_t)entry * K;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // (the first CTA runs before anything is sent to it: waited for below)
 
     grid_dependency_wait();             // logits, scores and flags may come from the preceding kernel of the stream
+    const int chunks = hi > lo ? (hi - lo + CHUNK - 1) / CHUNK : 0;
+    constexpr bool AHEAD = PT <= 12;    // a second piece in registers, fetched while one is worked on; with longer ones the SM's other CTAs have to do
+    float cur[PT], nxt[AHEAD ? PT : 1];
+    auto load = [&](float (&v)[PT], int b, int c) {
+        const int first = lo + c * CHUNK + at_group;
+        const float* z = p.logits + (row0 + b) * p.ld + first;
+        if (lo + (c + 1) * CHUNK <= hi) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i) v[i] = __ldcg(z + i * THREADS);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PT; ++i) v[i] = first + i * THREADS < hi ? __ldcg(z + i * THREADS) : -INFINITY;
+        }
+    };
+    if (chunks && group < K) load(cur, group, 0);           // (whether it counts is not known yet)
     for (int b = tid; b < K; b += nthreads) {
         s_score[b] = p.scores[row0 + b];
         s_done[b] = p.finished ? p.finished[row0 + b] != 0 : 0;
@@ -110,87 +169,108 @@ beam_select_kernel(SelectParams p)
     }
     __syncthreads();
 
-    // a row is read where its candidates can have a score
+    // a row is looked at where its candidates can have a score
     auto open = [&](int b) { return !s_done[b] && isfinite(s_score[b]); };
-    const int chunks = hi > lo ? (hi - lo + CHUNK - 1) / CHUNK : 0;
-    float cur[PT];
-    auto load = [&](int b, int c) {
-        const float* z = p.logits + (row0 + b) * p.ld;
-        const int first = lo + c * CHUNK + at_group;
-#pragma unroll
-        for (int i = 0; i < PT; ++i) cur[i] = first + i * THREADS < hi ? __ldcg(z + first + i * THREADS) : -INFINITY;
-    };
     auto next_open = [&](int b) { while (b < K && !open(b)) b += groups; return b; };
+    WarpSum* const sums_there = cluster.map_shared_rank(s.sums, 0) + rank * WARPS;
+    unsigned long long* const best_there = cluster.map_shared_rank(s.best, 0) + (size_t)rank * K;
 
-    for (int b = tid; b < K; b += nthreads)
-        if (chunks == 0 || !open(b))
-            for (int w = 0; w < WARPS; ++w) s.sums[b * WARPS + w] = {-INFINITY, 0.0f};
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (chunks == 0)
+        for (int i = tid; i < K * WARPS; i += nthreads) sums_there[i / WARPS * SLICES * WARPS + i % WARPS] = {-INFINITY, 0.0f};
     int b = chunks ? next_open(group) : K, c = 0, buffer = 0;
-    if (b < K) load(b, 0);
+    if (b < K && b != group) load(cur, b, 0);
     float m = -INFINITY, sum = 0.0f;
     uint32_t bound = 0;                 // below every logit that counts
-    while (b < K) {
+    // one piece, and the next one's loads
+    auto step = [&](float (&now)[PT], auto& next) {
+        int nb = b, nc = c + 1;
+        if (nc == chunks) { nc = 0; nb = next_open(b + groups); }
+        if constexpr (AHEAD) { if (nb < K) load(next, nb, nc); }
         // largest and sum of exponentials of this thread's share so far
-        float top = cur[0];
+        float top = now[0];
 #pragma unroll
-        for (int i = 1; i < PT; ++i) top = fmaxf(top, cur[i]);
+        for (int i = 1; i < PT; ++i) top = fmaxf(top, now[i]);
         const uint32_t v = top > -INFINITY ? ordered(top) : 0u;
-        uint32_t eight = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
-        eight = max(eight, __shfl_xor_sync(0xffffffffu, eight, 2));
-        eight = max(eight, __shfl_xor_sync(0xffffffffu, eight, 4));
-        if ((lane & 7) == 0) s_maxima[group][buffer][at_group >> 3] = eight;
-        const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.0f : m_new;
-        sum *= __expf(m - ref);
+        // (a row's second piece goes by the first one's bound: it would rarely raise it)
+        if (c != 1) {
+            uint32_t of_some = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
+            of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, 2));
+            if (THREADS == 256) of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, 4));
+            if ((lane & (THREADS / 32 - 1)) == 0) s_maxima[group][buffer][at_group / (THREADS / 32)] = of_some;
+        }
+        const float m_new = fmaxf(m, top * LOG2E), ref = m_new == -INFINITY ? 0.0f : m_new;
+        sum *= exp2_ftz(m - ref);
 #pragma unroll
-        for (int i = 0; i < PT; ++i) sum += __expf(cur[i] - ref);
+        for (int i = 0; i < PT; ++i) sum += exp2_ftz(fmaf(now[i], LOG2E, -ref));
         m = m_new;
-        asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
-        // (the two buffers in turn: who writes one again has passed the barrier behind everybody's reading of it)
-        uint32_t left = s_maxima[group][buffer][lane];
-        buffer ^= 1;
-        if (redux_max(left) > bound) {
-            uint32_t kth = 0;
-            for (int r = 0; r < K; ++r) {
-                kth = redux_max(left);
-                const uint32_t has = __ballot_sync(0xffffffffu, left == kth);
-                if (lane == __ffs(has) - 1) left = 0u;
+        if (c != 1) {
+            asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
+            // The bound: up to four beams the smallest of four maxima (of a quarter of the threads; 8 logits reach it on average, 50 once in a
+            // million), else the K-th of the 32, one by one (9 for eight beams).  The two buffers in turn: who writes one again has passed the barrier
+            // behind everybody's reading of it.
+            uint32_t left = s_maxima[group][buffer][lane];
+            buffer ^= 1;
+            if (K <= 4) {
+                left = max(left, __shfl_xor_sync(0xffffffffu, left, 4));
+                left = max(left, __shfl_xor_sync(0xffffffffu, left, 8));
+                left = max(left, __shfl_xor_sync(0xffffffffu, left, 16));
+                bound = max(bound, __reduce_min_sync(0xffffffffu, left));
+            } else if (redux_max(left) > bound) {
+                uint32_t kth = 0;
+                for (int r = 0; r < K; ++r) {
+                    kth = redux_max(left);
+                    const uint32_t has = __ballot_sync(0xffffffffu, left == kth);
+                    if (lane == __ffs(has) - 1) left = 0u;
+                }
+                bound = max(bound, kth);
             }
-            bound = max(bound, kth);
         }
         if (v && v >= bound) {
+            const float least = bound ? from_ordered(bound) : -3.402823466e38f;      // (no bound yet: everything but -inf)
 #pragma unroll
             for (int i = 0; i < PT; ++i) {
-                if (cur[i] > -INFINITY && ordered(cur[i]) >= bound) {
+                if (now[i] >= least) {
                     const int to = atomicAdd(&s.count[b], 1);
-                    if (to < CAP) s.list[b * CAP + to] = candidate(cur[i], lo + c * CHUNK + at_group + i * THREADS);
+                    if (to < CAP) s.list[b * CAP + to] = candidate(now[i], lo + c * CHUNK + at_group + i * THREADS);
                 }
             }
         }
-        int nb = b, nc = c + 1;
-        if (nc == chunks) { nc = 0; nb = next_open(b + groups); }
-        if (nb < K) load(nb, nc);
+        if constexpr (!AHEAD) { if (nb < K) load(now, nb, nc); }
         if (nb != b) {                  // the row is through: the warp's share of its sum
             const uint32_t wm = redux_max(m > -INFINITY ? ordered(m) : 0u);
             const float M = wm ? from_ordered(wm) : -INFINITY;
-            float t = sum * __expf(m - (wm ? M : 0.0f));        // (nothing but -inf: 0)
+            float t = sum * exp2_ftz(m - (wm ? M : 0.0f));        // (nothing but -inf: 0)
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-            if (lane == 0) s.sums[b * WARPS + warp] = {M, t};
+            if (lane == 0) sums_there[b * SLICES * WARPS + warp] = {M, t};
             m = -INFINITY; sum = 0.0f; bound = 0;
         }
         b = nb; c = nc;
+    };
+    while (b < K) {
+        step(cur, nxt);
+        if constexpr (AHEAD) { if (b < K) step(nxt, cur); }
     }
     __syncthreads();
 
     // the K best of each beam's slice, in order: a candidate's place is the number of candidates before it
     for (int q = tid >> 5; q < K; q += nthreads >> 5) {
         const int n = s.count[q];
-        unsigned long long* best = s.best + (size_t)q * K;
-        if (n <= CAP) {
+        unsigned long long* best = best_there + (size_t)q * SLICES * K;
+        if (n <= 32) {                  // (as a rule)
+            const unsigned long long mine = lane < n ? s.list[q * CAP + lane] : 0ull;
+            int before = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) before += __shfl_sync(0xffffffffu, mine, j) > mine;
+            if (before < K && mine) best[before] = mine;
+            if (lane >= n && lane < K) best[lane] = 0;
+        } else if (n <= CAP) {
             for (int r = (n < K ? n : K) + lane; r < K; r += 32) best[r] = 0;
             for (int i = lane; i < n; i += 32) {
                 const unsigned long long mine = s.list[q * CAP + i];
                 int place = 0;
+#pragma unroll 4
                 for (int j = 0; j < n; ++j) place += s.list[q * CAP + j] > mine;
                 if (place < K) best[place] = mine;
             }
@@ -215,80 +295,48 @@ beam_select_kernel(SelectParams p)
             }
         }
     }
-    cluster.sync();
-    if (rank == 0) {
-        // log-sum-exp of each row, from the 64 warps' shares, in double
-        for (int q = tid >> 5; q < K; q += nthreads >> 5) {
-            float wm[2], ws[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int w = lane + 32 * h;
-                const WarpSum* there = cluster.map_shared_rank(s.sums, w / WARPS);
-                wm[h] = there[q * WARPS + w % WARPS].m; ws[h] = there[q * WARPS + w % WARPS].s;
-            }
-            float M = fmaxf(wm[0], wm[1]);
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-            double t = 0.0;
-            if (isfinite(M)) t = (double)ws[0] * exp((double)wm[0] - M) + (double)ws[1] * exp((double)wm[1] - M);
-            else t = NAN;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-            if (lane == 0) s_lse[q] = (double)M + log(t);
-        }
-        if (tid == 0) { s_found = 0; s_cut = -INFINITY; s_cut_pair = 0x7fffffff; }
-        __syncthreads();
-        // every candidate's score; a beam's lists lie one behind the other, [beam][slice][place]
-        const int all = K * SLICES * K;
-        for (int i = tid; i < all; i += nthreads) {
-            const int q = i / (SLICES * K), slice = i / K % SLICES, r = i % K;
-            double total = -INFINITY;
-            int pair = 0x7fffffff;
-            if (open(q)) {
-                const unsigned long long k = cluster.map_shared_rank(s.best, slice)[q * K + r];
-                const double lse = s_lse[q];
-                if (k && isfinite(lse)) {
-                    total = (double)s_score[q] + ((double)from_ordered((uint32_t)(k >> 32)) - lse);
-                    pair = q * p.vocab + (int)~(uint32_t)k;
-                }
-            } else if (s_done[q] && slice == 0 && r == 0 && isfinite(s_score[q])) {
-                total = (double)s_score[q];
-                pair = q * p.vocab + p.eos;
-            }
-            s.total[i] = total; s.pair[i] = pair;
-        }
-    }
-    cluster.sync();                     // nobody's shared memory is read any more
-    if (rank != 0) return;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (rank != 0) return;              // (nobody reads another CTA's shared memory, and the first one stays)
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
-    // The K-th best of the lists' heads bounds what can be chosen: at most K lists reach it.  (Heads without a candidate are all alike and last.)
-    const int heads = K * SLICES;
-    for (int i = tid; i < heads; i += nthreads) {
-        const double mine = s.total[i * K];
-        const int pair = s.pair[i * K];
-        if (pair == 0x7fffffff) continue;
-        int place = 0;
-        for (int j = 0; j < heads; ++j) place += before(s.total[j * K], s.pair[j * K], mine, pair);
-        if (place == K - 1) { s_cut = mine; s_cut_pair = pair; }
+    // log-sum-exp of each row, from the warps' shares, summed in double
+    for (int q = tid >> 5; q < K; q += nthreads >> 5) {
+        if (!open(q)) continue;
+        constexpr int SHARES = SLICES * WARPS / 32;
+        WarpSum w[SHARES];
+        float M = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < SHARES; ++x) { w[x] = s.sums[q * SLICES * WARPS + 32 * x + lane]; M = fmaxf(M, w[x].m); }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+        double t = isfinite(M) ? 0.0 : (double)NAN;
+#pragma unroll
+        for (int x = 0; x < SHARES; ++x) t += (double)(w[x].s * exp2f(w[x].m - M));
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+        if (lane == 0) s_lse[q] = (double)M / (double)LOG2E + log(t);
     }
     __syncthreads();
-    // candidates at or before the bound, written down (over the lists of this CTA, which have been read)
-    double* kept = reinterpret_cast<double*>(s.best);                       // [K * K] doubles
-    int* kept_pair = reinterpret_cast<int*>(s.list);                        // [K * CAP * 2] words: K * K fit
-    for (int i = tid; i < K * SLICES * K; i += nthreads) {
-        const int pair = s.pair[i];
-        if (pair == 0x7fffffff || before(s_cut, s_cut_pair, s.total[i], pair)) continue;
-        const int at = atomicAdd(&s_found, 1);
-        kept[at] = s.total[i]; kept_pair[at] = pair;
+    if (tid < 32) {
+        // a beam's lists lie one behind the other, [beam][slice][place]; a beam that has ended has one candidate
+        auto score_of = [&](int list, int place) {
+            const int q = list / SLICES;
+            if (open(q)) {
+                const unsigned long long k = s.best[(size_t)list * K + place];
+                const double lse = s_lse[q];
+                if (k && isfinite(lse))
+                    return Choice{ordered((double)s_score[q] + ((double)from_ordered((uint32_t)(k >> 32)) - lse)), q * p.vocab + (int)~(uint32_t)k};
+            } else if (s_done[q] && list % SLICES == 0 && place == 0 && isfinite(s_score[q])) {
+                return Choice{ordered((double)s_score[q]), q * p.vocab + p.eos};
+            }
+            return Choice{0ull, 0};
+        };
+        const int n = K <= 4 ? join_lists<1>(K, score_of, s_chosen, s_chosen_pair) : K <= 8 ? join_lists<2>(K, score_of, s_chosen, s_chosen_pair)
+                    : K <= 16 ? join_lists<4>(K, score_of, s_chosen, s_chosen_pair) : join_lists<8>(K, score_of, s_chosen, s_chosen_pair);
+        if (lane == 0) s_found = n;
     }
     __syncthreads();
     const int found = s_found;
-    for (int i = tid; i < found; i += nthreads) {
-        int place = 0;
-        for (int j = 0; j < found; ++j) place += before(kept[j], kept_pair[j], kept[i], kept_pair[i]);
-        if (place < K) { s_chosen[place] = kept[i]; s_chosen_pair[place] = kept_pair[i]; }
-    }
-    __syncthreads();
     if (tid == 0 && found < K) {        // fewer candidates than beams: the first pairs that are none, with a score of -inf
         int pair = 0;
         for (int r = found; r < K; ++r, ++pair) {
@@ -310,29 +358,38 @@ beam_select_kernel(SelectParams p)
     }
 }
 
-template <int PT>
+template <int THREADS, int PT>
 amq_status launch_select_as(const SelectParams& p, int batch, int groups, cudaStream_t st)
 {
     const size_t smem = select_smem(p.beams, nullptr, nullptr);
-    AMQ_CUDA_TRY(cudaFuncSetAttribute(beam_select_kernel<PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    AMQ_CUDA_TRY(launch_kernel(beam_select_kernel<PT>, dim3((unsigned)(batch * SLICES)), dim3((unsigned)(THREADS * groups)), smem, st, true, p));
+    auto kernel = beam_select_kernel<THREADS, PT>;
+    AMQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    AMQ_CUDA_TRY(launch_kernel(kernel, dim3((unsigned)(batch * SLICES)), dim3((unsigned)(THREADS * groups)), smem, st, true, p));
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;
+}
+
+template <int THREADS>
+amq_status launch_select_groups(const SelectParams& p, int batch, int groups, cudaStream_t st)
+{
+    if (groups > p.beams) groups = p.beams;
+    const int slice = (p.vocab + SLICES - 1) / SLICES, most = groups == 1 ? 24 : 12;
+    const int pieces = (slice + THREADS * most - 1) / (THREADS * most), words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
+    if (words <= 2) return launch_select_as<THREADS, 2>(p, batch, groups, st);
+    if (words <= 5) return launch_select_as<THREADS, 5>(p, batch, groups, st);
+    if (words <= 8) return launch_select_as<THREADS, 8>(p, batch, groups, st);
+    if (words <= 10) return launch_select_as<THREADS, 10>(p, batch, groups, st);
+    if (words <= 12) return launch_select_as<THREADS, 12>(p, batch, groups, st);
+    if (words <= 16) return launch_select_as<THREADS, 16>(p, batch, groups, st);
+    if (words <= 21) return launch_select_as<THREADS, 21>(p, batch, groups, st);
+    return launch_select_as<THREADS, 24>(p, batch, groups, st);
 }
 
 amq_status launch_select(const SelectParams& p, int batch, cudaStream_t st)
 {
     // beams at a time: as many as leave the CTAs of all entries on the GPU at once
-    int groups = batch * SLICES <= 148 ? MAX_GROUPS : batch * SLICES <= 296 ? 2 : 1;
-    if (groups > p.beams) groups = p.beams;
-    const int slice = (p.vocab + SLICES - 1) / SLICES, pieces = (slice + THREADS * 24 - 1) / (THREADS * 24);
-    const int words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
-    if (words <= 2) return launch_select_as<2>(p, batch, groups, st);
-    if (words <= 5) return launch_select_as<5>(p, batch, groups, st);
-    if (words <= 8) return launch_select_as<8>(p, batch, groups, st);
-    if (words <= 12) return launch_select_as<12>(p, batch, groups, st);
-    if (words <= 16) return launch_select_as<16>(p, batch, groups, st);
-    return launch_select_as<24>(p, batch, groups, st);
+    if (batch * SLICES <= 148) return p.beams > 4 ? launch_select_groups<128>(p, batch, 8, st) : launch_select_groups<256>(p, batch, 4, st);
+    return launch_select_groups<256>(p, batch, batch * SLICES <= 296 ? 2 : 1, st);
 }
 
 // ---- reordering ------------------------------------------------------------------------------------------------------

@@ -27,6 +27,7 @@ struct ResGemmParams {
 
 // Row stride of the results staged for the stores: 8 mod 32 words for two vectors (conflict-free in the m16n8 layout), 16-byte rows.
 constexpr int Y_LD = 132;
+constexpr int BIAS_BYTES = 2 * 128 * 4;     // POST: bias of a tile's rows, double-buffered
 // groups of eight vectors per epilogue thread: TB <= 64, or 32 (registers)
 __host__ __device__ constexpr int res_ng(int k_a) { return k_a <= 2 ? 2 : 1; }
 
@@ -48,6 +49,7 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
     uint32_t* table = reinterpret_cast<uint32_t*>(sAlpha + 2 * AMQ_MAX_K * 128);
     float* sY = reinterpret_cast<float*>(table + RES_TABLE);                        // [TB][Y_LD] results of a tile
     ResSync& sy = *reinterpret_cast<ResSync*>(sY + p.TB * Y_LD);
+    float* sBias = reinterpret_cast<float*>(&sy + 1);                               // POST: [2][128]
     const uint32_t sB = smem_u32(smem_raw);
 
     // this CTA's share of the (block, tile) list; a pass is the part of it that lies in one block of vectors
@@ -129,20 +131,42 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
             const int row = tile * 128 + (te & 127), plane = te >> 7;
             return plane < p.k_w && row < p.units ? __ldcg(p.Walpha + (size_t)row * p.k_w + plane) : 0.0f;
         };
+        auto bias_of = [&](int tile) {
+            const int row = tile * 128 + te;
+            return a.bias && te < 128 && row < p.units ? __ldcg(a.bias + row) : 0.0f;
+        };
         grid_dependency_wait();
         while (w < w_end) {
             const int bb = (int)(w / a.mtiles), tile0 = (int)(w % a.mtiles), tiles = pass_tiles(w);
-            float next_alpha = alpha_of(tile0);
+            float next_alpha = alpha_of(tile0), next_bias = POST ? bias_of(tile0) : 0.0f;
             load_block(bb);
             f32x2 beta[NG][KA];
             res_load_beta<R, KA, NG>(p, sBeta, sub, beta);
             for (int t = 0; t < tiles; ++t) {
                 float* sa = sAlpha + (t & 1) * AMQ_MAX_K * 128;
                 sa[te] = next_alpha;
+                if (POST && te < 128) sBias[(t & 1) * 128 + te] = next_bias;
                 if (res_epi_bar<R>(!ok)) { ok = false; break; }        // (also: everybody is past the tile before last, whose buffer this is)
-                if (t + 1 < tiles) next_alpha = alpha_of(tile0 + t + 1);
+                if (t + 1 < tiles) { next_alpha = alpha_of(tile0 + t + 1); if (POST) next_bias = bias_of(tile0 + t + 1); }
                 f32x2 y[NG][4];
                 ok = res_drain_tile<R, KA, NG>(p, sy, sa, quarter, sub, tmem, beta, drain, y);
+                if constexpr (POST) {
+                    if (ok) {
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            float v[8];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float bias = sBias[(t & 1) * 128 + rl + 8 * i];       // added here, in front of the activation
+                                unpack2(y[g][i], v[2 * i], v[2 * i + 1]);
+                                v[2 * i] += bias; v[2 * i + 1] += bias;
+                            }
+                            activate(v, a.activation);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[g][i] = pack2(v[2 * i], v[2 * i + 1]);
+                        }
+                    }
+                }
                 // Results leave through shared memory and three warps of their own: in this layout a store from the registers is four
                 // 32-byte pieces, and stores from the epilogue warps held them up for longer than a tile's MMAs take.
                 if (ok && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&sy.yempty), y_parity))) { *(volatile int*)&sy.failed = 1; ok = false; }
@@ -172,8 +196,60 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
             grid_dependency_wait();
             load_block(bb);
             const int last = p.batch - b0 < p.TB ? p.batch - b0 : p.TB;
+            auto store = [&](int e, int row, bool vec, const float4& v) {
+                float* out = a.y + (size_t)(b0 + e) * a.ldy + row;
+                if (vec) {
+                    *reinterpret_cast<float4*>(out) = v;
+                } else {
+                    if (row < p.units) out[0] = v.x;
+                    if (row + 1 < p.units) out[1] = v.y;
+                    if (row + 2 < p.units) out[2] = v.z;
+                    if (row + 3 < p.units) out[3] = v.w;
+                }
+            };
             for (int t = 0; t < tiles && ok; ++t) {
                 const int row = (tile0 + t) * 128 + 4 * lane;
+                const bool vec = VEC && row + 3 < p.units;
+                if constexpr (POST) {
+                    // The residual, a window of vectors ahead, of the next tile as far as L2: the stores may be over it (y = residual), so that the compiler
+                    // moves no load in front of one; every element is read by the thread that writes it, before.
+                    constexpr int WINDOW = 6;
+                    const int first = warp - R::MMA_WARP - 1;
+                    auto fetch = [&](int e) {
+                        float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (e >= last || !a.residual) return r;
+                        const float* res = a.residual + (size_t)(b0 + e) * a.ldr + row;
+                        if (vec) return __ldcg(reinterpret_cast<const float4*>(res));
+                        if (row < p.units) r.x = __ldcg(res);
+                        if (row + 1 < p.units) r.y = __ldcg(res + 1);
+                        if (row + 2 < p.units) r.z = __ldcg(res + 2);
+                        if (row + 3 < p.units) r.w = __ldcg(res + 3);
+                        return r;
+                    };
+                    float4 r[WINDOW];
+#pragma unroll
+                    for (int q = 0; q < WINDOW; ++q) r[q] = fetch(first + q * R::OUT_WARPS);
+                    if (a.residual && t + 1 < tiles && (lane & 7) == 0 && row + 128 < p.units)
+                        for (int e = first; e < last; e += R::OUT_WARPS)
+                            asm volatile("prefetch.global.L2 [%0];" :: "l"(a.residual + (size_t)(b0 + e) * a.ldr + row + 128));
+                    ok = __all_sync(0xffffffffu, mbar_wait_relaxed(smem_u32(&sy.yfull), y_parity, &sy.failed));
+                    y_parity ^= 1u;
+                    if (!ok) { *(volatile int*)&sy.failed = 1; break; }
+                    for (int e0 = first; e0 < last; e0 += WINDOW * R::OUT_WARPS) {
+#pragma unroll
+                        for (int q = 0; q < WINDOW; ++q) {
+                            const int e = e0 + q * R::OUT_WARPS;
+                            if (e >= last) break;
+                            float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
+                            v.x += r[q].x; v.y += r[q].y; v.z += r[q].z; v.w += r[q].w;
+                            r[q] = fetch(e + WINDOW * R::OUT_WARPS);
+                            store(e, row, vec, v);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(&sy.yempty)) : "memory");
+                    continue;
+                }
                 float4 bias = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (a.bias) {
                     if (row < p.units) bias.x = __ldcg(a.bias + row);
@@ -184,36 +260,11 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
                 ok = __all_sync(0xffffffffu, mbar_wait_relaxed(smem_u32(&sy.yfull), y_parity, &sy.failed));
                 y_parity ^= 1u;
                 if (!ok) { *(volatile int*)&sy.failed = 1; break; }
-                const bool vec = VEC && row + 3 < p.units;
 #pragma unroll 4
                 for (int e = warp - R::MMA_WARP - 1; e < last; e += R::OUT_WARPS) {
                     float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
                     v.x += bias.x; v.y += bias.y; v.z += bias.z; v.w += bias.w;
-                    if constexpr (POST) {
-                        float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (a.residual) {
-                            const float* res = a.residual + (size_t)(b0 + e) * a.ldr + row;
-                            if (vec) {
-                                r = __ldcg(reinterpret_cast<const float4*>(res));
-                            } else {
-                                if (row < p.units) r.x = __ldcg(res);
-                                if (row + 1 < p.units) r.y = __ldcg(res + 1);
-                                if (row + 2 < p.units) r.z = __ldcg(res + 2);
-                                if (row + 3 < p.units) r.w = __ldcg(res + 3);
-                            }
-                        }
-                        v.x = activate(v.x, a.activation) + r.x; v.y = activate(v.y, a.activation) + r.y;
-                        v.z = activate(v.z, a.activation) + r.z; v.w = activate(v.w, a.activation) + r.w;
-                    }
-                    float* out = a.y + (size_t)(b0 + e) * a.ldy + row;
-                    if (vec) {
-                        *reinterpret_cast<float4*>(out) = v;
-                    } else {
-                        if (row < p.units) out[0] = v.x;
-                        if (row + 1 < p.units) out[1] = v.y;
-                        if (row + 2 < p.units) out[2] = v.z;
-                        if (row + 3 < p.units) out[3] = v.w;
-                    }
+                    store(e, row, vec, v);
                 }
                 __syncwarp();
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(&sy.yempty)) : "memory");
@@ -251,7 +302,7 @@ bool plan(const GemmArgs& g, int sms, ResGemmPlan* out)
     double best = 0.0;
     for (int TB = 8; TB <= 8 * res_ng(g.k_a) * R::SPLIT; TB += 8) {
         ResProblem q = p;
-        if (!res_set_block<R>(q, TB, g.k_a, (size_t)TB * Y_LD * 4)) break;
+        if (!res_set_block<R>(q, TB, g.k_a, (size_t)TB * Y_LD * 4 + (g.post ? BIAS_BYTES : 0))) break;
         const long long blocks = (g.batch + TB - 1) / TB, per_cta = (blocks * a.mtiles + sms - 1) / sms;
         const double expand = (double)q.N * q.NS * 128 / 80.0 + 1500.0;
         const double t = (double)per_cta * q.k_w * q.NS * res_slot_clocks(q) + expand * (1.0 + (double)per_cta / a.mtiles);
@@ -263,7 +314,7 @@ bool plan(const GemmArgs& g, int sms, ResGemmPlan* out)
     a.xcodes = g.xcodes; a.xbeta = g.xbeta; a.bias = g.bias; a.y = g.y; a.ldy = g.ldy;
     const long long total = (long long)a.blocks * a.mtiles;
     out->grid = (int)(total < sms ? total : sms);
-    out->smem = res_smem_bytes(a.p) + (size_t)a.p.TB * Y_LD * 4;
+    out->smem = res_smem_bytes(a.p) + (size_t)a.p.TB * Y_LD * 4 + (g.post ? BIAS_BYTES : 0);
     a.early_weights = !g.from_entry;
     a.activation = g.activation; a.residual = g.residual; a.ldr = g.ldr;
     out->vec_out = aligned16(g.y) && g.ldy % 4 == 0 && (!g.residual || (aligned16(g.residual) && g.ldr % 4 == 0));

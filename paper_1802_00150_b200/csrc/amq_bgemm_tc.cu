@@ -443,8 +443,9 @@ __device__ __forceinline__ void epilogue_smem_to_global(const TcParams& p, const
                         if (b4 + 2 < bend) r.z = __ldcg(res + 2 * (size_t)a.ldr);
                         if (b4 + 3 < bend) r.w = __ldcg(res + 3 * (size_t)a.ldr);
                     }
-                    s.x = activate(s.x, a.activation) + r.x; s.y = activate(s.y, a.activation) + r.y;
-                    s.z = activate(s.z, a.activation) + r.z; s.w = activate(s.w, a.activation) + r.w;
+                    float v[4] = {s.x, s.y, s.z, s.w};
+                    activate(v, a.activation);
+                    s = make_float4(v[0] + r.x, v[1] + r.y, v[2] + r.z, v[3] + r.w);
                 }
                 out[(size_t)b4 * a.ldy] = s.x;
                 if (b4 + 1 < bend) out[(size_t)(b4 + 1) * a.ldy] = s.y;

@@ -24,7 +24,7 @@ amq_status launch_binary_gemv(const GemmArgs& a, cudaStream_t st)
     p.D = a.D;
     p.m = a.m; p.n = a.n; p.CH = words_per_row(a.n) / 4;
     p.epilogue = a.epilogue;
-    p.overlap = a.overlap_with_previous;
+    p.overlap = a.overlap_with_previous || (a.post && a.from_entry);    // (the kernel waits before it reads anything)
     p.xf = nullptr; p.T = 0; p.xcodes_out = nullptr; p.xbeta_out = nullptr;
     p.activation = a.activation; p.residual = a.residual;
     return a.post ? launch_bgemv_post(p, a.k_w, a.k_a, st) : launch_kw<false>(p, a.k_w, a.k_a, st);

@@ -10,11 +10,15 @@
 
 #include <dlfcn.h>
 
+#include <algorithm>
+#include <climits>
 #include <tuple>
 #include <type_traits>
 #include <utility>
 
 #include <ATen/ATen.h>
+#include <c10/core/Storage.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -110,6 +114,259 @@ PyObject* call(amq_status (*f)(A...), PyObject* const* args, Py_ssize_t nargs)
     PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return call(p_##name, args, nargs); }
 AMQ_ENTRIES(AMQ_WRAP)
 
+// ---- calls whose arguments are looked at and whose results are made here as well -----------------------------------------------------
+// (short kernels: shapes, strides and results cost the interpreter more than the kernel takes).  Each answers with its results, or with the status
+// of a call that the library refused, as an integer.
+
+// a tensor argument, or null (with a Python error) where it is none
+const at::Tensor* tensor(PyObject* o, const char* name)
+{
+    if (THPVariable_Check(o)) return &THPVariable_Unpack(o);
+    PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
+    return nullptr;
+}
+
+bool refuse(const char* what) { PyErr_SetString(PyExc_TypeError, what); return false; }
+
+bool shaped(const at::Tensor& t, at::ScalarType type, std::initializer_list<int64_t> shape)
+{
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != (int64_t)shape.size()) return false;
+    int64_t d = 0;
+    for (int64_t s : shape)
+        if (t.size(d++) != s) return false;
+    return true;
+}
+
+// the same, and contiguous
+bool packed(const at::Tensor& t, at::ScalarType type, std::initializer_list<int64_t> shape) { return shaped(t, type, shape) && t.is_contiguous(); }
+
+// rows of a matrix: contiguous, at any stride that is no shorter; their stride, or -1
+int64_t leading(const at::Tensor& t)
+{
+    const int64_t rows = t.size(0), cols = t.size(1);
+    if (cols > 1 && t.stride(1) != 1) return -1;
+    if (rows <= 1) return std::max(cols, t.stride(0));
+    return t.stride(0) >= cols ? t.stride(0) : -1;
+}
+
+bool same_device(std::initializer_list<const at::Tensor*> ts)
+{
+    const at::Tensor* first = nullptr;
+    for (const at::Tensor* t : ts) {
+        if (!t) continue;
+        if (first && t->device() != first->device()) return refuse("all tensors must be on one device");
+        first = t;
+    }
+    return true;
+}
+
+int64_t fits(int64_t v) { return v <= INT_MAX ? v : -1; }       // (a size that the library refuses)
+
+at::Tensor fresh(at::IntArrayRef size, at::ScalarType type, const at::Tensor& like) { return at::empty(size, at::TensorOptions().dtype(type).device(like.device())); }
+
+template <typename F>
+PyObject* guarded(F&& f)
+{
+    try {
+        return f();
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// the device of the call's tensors made current, and its current stream
+struct On {
+    c10::cuda::CUDAGuard guard;
+    explicit On(const at::Tensor& t) : guard(t.device()) {}
+    void* stream() const { return c10::cuda::getCurrentCUDAStream().stream(); }
+};
+
+// binary_gemm_act(Wcodes, Walpha, xcodes, xbeta, n, bias, activation, residual, y)
+PyObject* py_binary_gemm_act(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    if (!p_amq_binary_gemm_act || nargs != 9) { PyErr_SetString(PyExc_TypeError, "binary_gemm_act takes nine arguments of an opened library"); return nullptr; }
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *Wc = tensor(args[0], "Wcodes"), *Wa = Wc ? tensor(args[1], "Walpha") : nullptr, *xc = Wa ? tensor(args[2], "xcodes") : nullptr,
+                         *xb = xc ? tensor(args[3], "xbeta") : nullptr;
+        if (!xb) return nullptr;
+        const at::Tensor *bias = nullptr, *residual = nullptr, *y = nullptr;
+        if (args[5] != Py_None && !(bias = tensor(args[5], "bias"))) return nullptr;
+        if (args[7] != Py_None && !(residual = tensor(args[7], "residual"))) return nullptr;
+        if (args[8] != Py_None && !(y = tensor(args[8], "y"))) return nullptr;
+        const long long n = PyLong_AsLongLong(args[4]), act = PyLong_AsLongLong(args[6]);
+        if (PyErr_Occurred()) return nullptr;
+        if (Wc->dim() != 3 || xc->dim() != 3) { refuse("codes must have the shape (rows, bits, words of a plane)"); return nullptr; }
+        const int64_t m = Wc->size(0), kw = Wc->size(1), batch = xc->size(0), ka = xc->size(1), words = 4 * ((n + 127) / 128);
+        if (!packed(*Wc, at::kInt, {m, kw, words}) || !packed(*xc, at::kInt, {batch, ka, words})) {
+            refuse("codes must be contiguous CUDA int32 tensors (rows, bits, words of a plane of n)");
+            return nullptr;
+        }
+        if (!packed(*Wa, at::kFloat, {m, kw}) || !packed(*xb, at::kFloat, {batch, ka}) || (bias && !packed(*bias, at::kFloat, {m}))) {
+            refuse("coefficients (rows, bits) and bias (rows of W) must be contiguous CUDA float32 tensors");
+            return nullptr;
+        }
+        if ((residual && (!shaped(*residual, at::kFloat, {batch, m}) || leading(*residual) < 0)) || (y && (!shaped(*y, at::kFloat, {batch, m}) || leading(*y) < 0))) {
+            refuse("residual and y must be CUDA float32 tensors (vectors, rows of W) with contiguous rows");
+            return nullptr;
+        }
+        if (!same_device({Wc, Wa, xc, xb, bias, residual, y})) return nullptr;
+        const On on(*Wc);
+        at::Tensor out = y ? *y : fresh({batch, m}, at::kFloat, *Wc);
+        const amq_status s = p_amq_binary_gemm_act(
+            static_cast<const uint32_t*>(Wc->data_ptr()), static_cast<const float*>(Wa->data_ptr()), (int)fits(m), (int)fits(n), (int)kw,
+            static_cast<const uint32_t*>(xc->data_ptr()), static_cast<const float*>(xb->data_ptr()), (int)fits(batch), (int)ka,
+            bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, (int)act, residual ? static_cast<const float*>(residual->data_ptr()) : nullptr,
+            residual ? (int)fits(leading(*residual)) : 0, static_cast<float*>(out.data_ptr()), (int)fits(leading(out)), on.stream());
+        return s == AMQ_OK ? THPVariable_Wrap(out) : PyLong_FromLong(s);
+    });
+}
+
+// a cache (kcodes, kcoeffs, vcodes, vcoeffs), block table and lengths, checked against one another
+struct Cache {
+    const at::Tensor *t[4], *table, *lengths;
+    int64_t pages, page_size, heads, k, d, batch, max_pages, ld_table;
+};
+
+bool cache_of(PyObject* cache, PyObject* table, PyObject* lengths, int64_t d, Cache* out)
+{
+    if (!PyTuple_Check(cache) && !PyList_Check(cache)) return refuse("a cache is (kcodes, kcoeffs, vcodes, vcoeffs)");
+    if (PySequence_Fast_GET_SIZE(cache) != 4) return refuse("a cache is (kcodes, kcoeffs, vcodes, vcoeffs)");
+    for (int i = 0; i < 4; ++i)
+        if (!(out->t[i] = tensor(PySequence_Fast_GET_ITEM(cache, i), "each part of a cache"))) return false;
+    if (!(out->table = tensor(table, "table")) || !(out->lengths = tensor(lengths, "lengths"))) return false;
+    const at::Tensor& k = *out->t[0];
+    if (k.dim() != 5) return refuse("cached codes must have the shape (pages, page_size, heads, bits, words of a plane)");
+    out->pages = k.size(0); out->page_size = k.size(1); out->heads = k.size(2); out->k = k.size(3); out->d = d;
+    const int64_t words = 4 * ((d + 127) / 128);
+    for (int i = 0; i < 4; ++i) {
+        const bool ok = i % 2 == 0 ? packed(*out->t[i], at::kInt, {out->pages, out->page_size, out->heads, out->k, words})
+                                   : packed(*out->t[i], at::kFloat, {out->pages, out->page_size, out->heads, out->k});
+        if (!ok) return refuse("a cache is four contiguous CUDA tensors: int32 codes (pages, page_size, heads, bits, words of a plane of d), float32 coefficients "
+                               "(pages, page_size, heads, bits), of the keys and of the values");
+    }
+    const at::Tensor& t = *out->table;
+    if (!t.is_cuda() || t.scalar_type() != at::kInt || t.dim() != 2 || leading(t) < 0)
+        return refuse("table must be a CUDA int32 tensor (batch, pages of a sequence) with contiguous rows");
+    out->batch = t.size(0); out->max_pages = t.size(1); out->ld_table = leading(t);
+    if (!packed(*out->lengths, at::kInt, {out->batch})) return refuse("lengths must be a contiguous CUDA int32 tensor (batch,)");
+    return same_device({out->t[0], out->t[1], out->t[2], out->t[3], out->table, out->lengths});
+}
+
+template <typename T> T* data(const at::Tensor* t) { return static_cast<T*>(t->data_ptr()); }
+
+// cache_append(kcodes, kcoeffs, vcodes, vcoeffs, cache, table, lengths, d)
+PyObject* py_cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    if (!p_amq_cache_append || nargs != 8) { PyErr_SetString(PyExc_TypeError, "cache_append takes eight arguments of an opened library"); return nullptr; }
+    return guarded([&]() -> PyObject* {
+        const long long d = PyLong_AsLongLong(args[7]);
+        Cache c;
+        if (PyErr_Occurred() || !cache_of(args[4], args[5], args[6], d, &c)) return nullptr;
+        const at::Tensor* rows[4];
+        for (int i = 0; i < 4; ++i)
+            if (!(rows[i] = tensor(args[i], "each of the new rows' parts"))) return nullptr;
+        const int64_t count = rows[0]->dim() == 5 ? rows[0]->size(1) : -1, words = 4 * ((d + 127) / 128);
+        for (int i = 0; i < 4; ++i) {
+            const bool ok = i % 2 == 0 ? packed(*rows[i], at::kInt, {c.batch, count, c.heads, c.k, words}) : packed(*rows[i], at::kFloat, {c.batch, count, c.heads, c.k});
+            if (!ok) { refuse("new rows are contiguous CUDA tensors (batch, count, heads, bits[, words of a plane]), as the cache and the table have them"); return nullptr; }
+        }
+        if (!same_device({c.t[0], rows[0], rows[1], rows[2], rows[3]})) return nullptr;
+        const On on(*c.t[0]);
+        return PyLong_FromLong(p_amq_cache_append(data<const uint32_t>(rows[0]), data<const float>(rows[1]), data<const uint32_t>(rows[2]), data<const float>(rows[3]),
+                                                  data<uint32_t>(c.t[0]), data<float>(c.t[1]), data<uint32_t>(c.t[2]), data<float>(c.t[3]),
+                                                  (int)fits(c.pages), (int)fits(c.page_size), (int)fits(c.heads), (int)fits(d), (int)c.k, data<const int32_t>(c.table),
+                                                  (int)fits(c.ld_table), (int)fits(c.max_pages), data<const int32_t>(c.lengths), (int)fits(c.batch), (int)fits(count),
+                                                  on.stream()));
+    });
+}
+
+decltype(&::amq_cache_attention_workspace_bytes) p_amq_cache_attention_workspace_bytes = nullptr;
+
+// cache_attention(q, cache, table, lengths, scale, workspace, out)
+PyObject* py_cache_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    if (!p_amq_cache_attention || nargs != 7) { PyErr_SetString(PyExc_TypeError, "cache_attention takes seven arguments of an opened library"); return nullptr; }
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* q = tensor(args[0], "q");
+        if (!q) return nullptr;
+        if (!q->is_cuda() || q->scalar_type() != at::kFloat || q->dim() != 4 || (q->size(3) > 1 && q->stride(3) != 1)) {
+            refuse("q must be a CUDA float32 tensor (batch, q_len, q_heads, d) with contiguous rows");
+            return nullptr;
+        }
+        const int64_t batch = q->size(0), q_len = q->size(1), q_heads = q->size(2), d = q->size(3);
+        Cache c;
+        if (!cache_of(args[1], args[2], args[3], d, &c)) return nullptr;
+        if (c.batch != batch) { refuse("q and table must agree in their first dimension"); return nullptr; }
+        const float scale = (float)PyFloat_AsDouble(args[4]);
+        if (PyErr_Occurred()) return nullptr;
+        const at::Tensor *workspace = nullptr, *given = nullptr;
+        if (args[5] != Py_None && !(workspace = tensor(args[5], "workspace"))) return nullptr;
+        if (args[6] != Py_None && !(given = tensor(args[6], "out"))) return nullptr;
+        if (workspace && (!workspace->is_cuda() || !workspace->is_contiguous())) { refuse("workspace must be a contiguous CUDA tensor"); return nullptr; }
+        if (given && !packed(*given, at::kFloat, {batch, q_len, q_heads, d})) { refuse("out must be a contiguous CUDA float32 tensor of q's shape"); return nullptr; }
+        if (!same_device({q, c.t[0], workspace, given})) return nullptr;
+        const On on(*q);
+        at::Tensor own, out = given ? *given : fresh({batch, q_len, q_heads, d}, at::kFloat, *q);
+        if (!workspace) {
+            const size_t bytes = p_amq_cache_attention_workspace_bytes((int)fits(batch), (int)fits(q_len), (int)fits(q_heads), (int)fits(c.heads), (int)fits(d),
+                                                                       (int)fits(c.max_pages * c.page_size));
+            if (bytes) { own = fresh({(int64_t)bytes}, at::kByte, *q); workspace = &own; }
+        }
+        const amq_status s = p_amq_cache_attention(
+            data<const float>(q), q->stride(0), q->stride(1), q->stride(2), data<const uint32_t>(c.t[0]), data<const float>(c.t[1]), data<const uint32_t>(c.t[2]),
+            data<const float>(c.t[3]), (int)fits(c.pages), (int)fits(c.page_size), (int)fits(c.heads), (int)fits(d), (int)c.k, data<const int32_t>(c.table),
+            (int)fits(c.ld_table), (int)fits(c.max_pages), data<const int32_t>(c.lengths), (int)fits(batch), (int)fits(q_len), (int)fits(q_heads), scale,
+            static_cast<float*>(out.data_ptr()), workspace ? workspace->data_ptr() : nullptr, workspace ? workspace->nbytes() : 0, on.stream());
+        return s == AMQ_OK ? THPVariable_Wrap(out) : PyLong_FromLong(s);
+    });
+}
+
+// a contiguous part of a buffer as a tensor of its own
+PyObject* part_of(const at::Tensor& buffer, int64_t first, at::IntArrayRef size, at::ScalarType type)
+{
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_storage_offset(first);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return THPVariable_Wrap(t);
+}
+
+// beam_select(logits, scores, finished, eos) -> (scores, parents, tokens, finished), four parts of one allocation
+PyObject* py_beam_select(PyObject*, PyObject* const* args, Py_ssize_t nargs)
+{
+    if (!p_amq_beam_select || nargs != 4) { PyErr_SetString(PyExc_TypeError, "beam_select takes four arguments of an opened library"); return nullptr; }
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *logits = tensor(args[0], "logits"), *scores = logits ? tensor(args[1], "scores") : nullptr, *finished = nullptr;
+        if (!scores || (args[2] != Py_None && !(finished = tensor(args[2], "finished")))) return nullptr;
+        const long long eos = PyLong_AsLongLong(args[3]);
+        if (PyErr_Occurred()) return nullptr;
+        if (scores->dim() != 2 || !packed(*scores, at::kFloat, {scores->size(0), scores->size(1)})) {
+            refuse("scores must be a contiguous CUDA float32 tensor (batch, beams)");
+            return nullptr;
+        }
+        const int64_t batch = scores->size(0), beams = scores->size(1);
+        if (logits->dim() != 2 || !shaped(*logits, at::kFloat, {batch * beams, logits->size(1)}) || leading(*logits) < 0) {
+            refuse("logits must be a CUDA float32 tensor (batch * beams, vocabulary) with contiguous rows");
+            return nullptr;
+        }
+        if (finished && !packed(*finished, at::kInt, {batch, beams})) { refuse("finished must be a contiguous CUDA int32 tensor (batch, beams)"); return nullptr; }
+        if (!same_device({logits, scores, finished})) return nullptr;
+        const On on(*scores);
+        const int64_t n = batch * beams, step = (n + 3) / 4 * 4;         // (each part on 16 bytes)
+        at::Tensor buffer = fresh({4 * step}, at::kInt, *scores);
+        int32_t* at = static_cast<int32_t*>(buffer.data_ptr());
+        const amq_status s = p_amq_beam_select(data<const float>(logits), (int)fits(leading(*logits)), (int)fits(logits->size(1)), data<const float>(scores),
+                                               finished ? data<const int32_t>(finished) : nullptr, eos == (int)eos ? (int)eos : -2, (int)fits(batch), (int)fits(beams),
+                                               reinterpret_cast<float*>(at), at + step, at + 2 * step, at + 3 * step, on.stream());
+        if (s != AMQ_OK) return PyLong_FromLong(s);
+        PyObject* parts[4];
+        for (int i = 0; i < 4; ++i) parts[i] = part_of(buffer, i * step, {batch, beams}, i == 0 ? at::kFloat : at::kInt);
+        PyObject* answer = PyTuple_Pack(4, parts[0], parts[1], parts[2], parts[3]);
+        for (PyObject* q : parts) Py_XDECREF(q);
+        return answer;
+    });
+}
+
 // amq_beam_reorder(states, out, parents): two sequences of tensors (batch, beams, ..), rows contiguous and at one stride, and the parents;
 // the call's HOST arrays are made from them here
 decltype(&::amq_beam_reorder) p_amq_beam_reorder = nullptr;
@@ -173,7 +430,8 @@ PyObject* py_amq_beam_reorder(PyObject*, PyObject* const* args, Py_ssize_t nargs
                     }
                 }
                 if (ok) {
-                    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+                    const On on(parents);
+                    void* stream = on.stream();
                     amq_status s;
                     Py_BEGIN_ALLOW_THREADS
                     s = p_amq_beam_reorder(src, dst, bytes, from, to, (int)count, static_cast<const int32_t*>(parents.data_ptr()), (int)parents.size(0),
@@ -204,6 +462,7 @@ PyObject* py_open(PyObject*, PyObject* path)
     if (!p_##name) { PyErr_SetString(PyExc_ImportError, "missing entry point " #name); return nullptr; }
     AMQ_ENTRIES(AMQ_LOOKUP)
     AMQ_LOOKUP(amq_beam_reorder)
+    AMQ_LOOKUP(amq_cache_attention_workspace_bytes)
     Py_RETURN_NONE;
 }
 
@@ -232,6 +491,7 @@ PyObject* py_empty(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 PyMethodDef methods[] = {
     AMQ_ENTRIES(AMQ_METHOD)
     AMQ_METHOD(amq_beam_reorder)
+    AMQ_METHOD(binary_gemm_act) AMQ_METHOD(cache_append) AMQ_METHOD(cache_attention) AMQ_METHOD(beam_select)
     {"open", py_open, METH_O, nullptr},
     {"empty", (PyCFunction)(void (*)(void))py_empty, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

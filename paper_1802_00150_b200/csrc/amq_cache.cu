@@ -3,13 +3,14 @@
 //   s[t] = scale * sum_i a[t][i] (q . b[t][i]),   p = softmax over the visible t,   o = sum_t p[t] sum_i a'[t][i] b'[t][i]
 // with the planes b, b' (+-1) and coefficients a, a' of token t's key and value.
 #include "amq_common.cuh"
+#include "amq_pairs.cuh"
 
 namespace amq {
 namespace {
 
 struct CacheView {
     const uint32_t* kcodes; const float* kcoeffs; const uint32_t* vcodes; const float* vcoeffs;
-    int pages, page_size, heads, d, k, wpr;
+    int pages, page_size, page_shift, heads, d, k, wpr;     // page_shift: of a page size that is a power of two, else -1
     const int32_t* table; int ld_table, max_pages;
     const int32_t* lengths;
 };
@@ -22,10 +23,11 @@ __device__ __forceinline__ int visible_length(const CacheView& c, int b)
 }
 
 // slot (token position in the whole cache) of token t of sequence b, -1 where the table names no page
-__device__ __forceinline__ long long slot_of(const CacheView& c, int b, int t)
+__device__ __forceinline__ int slot_of(const CacheView& c, int b, int t)
 {
-    const int page = c.table[(size_t)b * c.ld_table + t / c.page_size];
-    return page >= 0 && page < c.pages ? (long long)page * c.page_size + t % c.page_size : -1;
+    const int j = c.page_shift >= 0 ? t >> c.page_shift : t / c.page_size;
+    const int page = c.table[(size_t)b * c.ld_table + j];
+    return page >= 0 && page < c.pages ? page * c.page_size + (t - j * c.page_size) : -1;
 }
 
 struct AppendParams {
@@ -43,7 +45,7 @@ cache_append_kernel(const __grid_constant__ AppendParams p)
     const int b = blockIdx.x / p.count, i = blockIdx.x % p.count;
     const int t = p.c.lengths[b] - p.count + i;
     if (t < 0 || t >= (long long)p.c.max_pages * p.c.page_size) return;
-    const long long slot = slot_of(p.c, b, t);
+    const int slot = slot_of(p.c, b, t);
     if (slot < 0) return;
     const int rows = p.c.heads * p.c.k, chunks = rows * (p.c.wpr / 4);
     const size_t from = blockIdx.x, to = (size_t)slot;
@@ -71,7 +73,13 @@ struct AttentionParams {
 
 constexpr int WARPS = 4;
 constexpr int TILE = 32;                // tokens
-constexpr int STAGES = 3;
+#ifndef AT_STAGES
+#define AT_STAGES 3
+#endif
+#ifndef AT_MINB
+#define AT_MINB 3
+#endif
+constexpr int STAGES = AT_STAGES;
 constexpr int ROWS = 4;                 // query rows of a CTA
 constexpr float MAGIC = 12582912.0f;    // 1.5 2^23: a float of this size holds an integer of 22 bits in its low bits
 constexpr int MAGIC_BITS = 0x4B400000;
@@ -82,6 +90,8 @@ template <int K> struct Stage {
     uint4 k[TILE * pitch(K)], v[TILE * pitch(K)];
     float ka[TILE * pitch(K)], va[TILE * pitch(K)];
 };
+// a tile's coefficients by planes
+template <int K> struct Coefficients { float k[K][TILE], v[K][TILE]; };
 // place of a token's plane: spread so that neither access pattern below meets a bank twice
 template <int K> __device__ __forceinline__ int place(int token, int plane)
 {
@@ -104,6 +114,17 @@ __device__ __forceinline__ void mma_s8u8(int (&c)[4], const uint32_t (&a)[4], ui
         : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// the first of a chain: the sum starts from `start`, whose registers stay (a constant in place would be moved there each time)
+__device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const int (&start)[4])
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(start[0]), "r"(start[1]), "r"(start[2]), "r"(start[3]));
+}
+
+// two sums as floats: integers of up to 22 bits on top of MAGIC
+__device__ __forceinline__ f32x2 sums2(int a, int b) { return add2(pack2(__int_as_float(a), __int_as_float(b)), pack2(-MAGIC, -MAGIC)); }
+
 __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // The products run on the integer tensor cores, on the planes' bits as they are stored: a word ANDed with 0x01010101 << j is four bytes of 0 or
@@ -120,7 +141,7 @@ __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx
 // word of the plane; results are those of tokens 2 c, 2 c + 1.  For values, c stands for the same two tokens, so weights never change
 // lanes, and column g for dimensions 16 g .. 16 g + 15, one per MMA.
 template <int K>
-__global__ void __launch_bounds__(WARPS * 32, 3)
+__global__ void __launch_bounds__(WARPS * 32, AT_MINB)
 cache_attention_kernel(const __grid_constant__ AttentionParams p)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -129,6 +150,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3, r = g & 3;
     const bool upper = g < 4;           // rows g, g + 8: digits 3 and 1 of the query (weights: 2 and 0), else 2 and 0 (1 and none)
     Stage<K>* stages = reinterpret_cast<Stage<K>*>(smem_raw) + warp * STAGES;
+    Coefficients<K>& coef = (reinterpret_cast<Coefficients<K>*>(reinterpret_cast<Stage<K>*>(smem_raw) + WARPS * STAGES))[warp];
 
     int at = blockIdx.x;
     const int rb = at % p.row_blocks; at /= p.row_blocks;
@@ -140,40 +162,42 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
     const int last_row = min(rb * ROWS + ROWS, p.rows) - 1;
     const int limit = max(length - p.q_len + 1 + last_row / p.group, 0);        // of the block's last row: no other sees more
     const int row = rb * ROWS + r;
-    const int my_limit = row < p.rows ? length - p.q_len + 1 + row / p.group : 0;
+    const int my_limit = row < p.rows ? length - p.q_len + 1 + row / p.group : limit;
     const int tiles = limit > 0 ? (limit - 1) / TILE + 1 : 0;
     const int tile0 = (int)((long long)tiles * split / p.splits), tile1 = (int)((long long)tiles * (split + 1) / p.splits);
 
     auto slot_at = [&](int tile) {
         const int t = tile * TILE + lane;
-        return tile < tile1 && t < limit ? slot_of(cv, b, t) : -1ll;
+        return tile < tile1 && t < limit ? slot_of(cv, b, t) : -1;
     };
-    auto issue = [&](Stage<K>& st, long long slot) {
-        const uint4* kc = reinterpret_cast<const uint4*>(cv.kcodes) + (size_t)kv * K;
-        const uint4* vc = reinterpret_cast<const uint4*>(cv.vcodes) + (size_t)kv * K;
-        const size_t step = (size_t)cv.heads * K;
+    // planes: K lanes a token, so that an instruction's lanes meet few lines; coefficients: a lane a token
+    const size_t step = (size_t)cv.heads * K;
+    const uint4* const kcodes = reinterpret_cast<const uint4*>(cv.kcodes) + (size_t)kv * K;
+    const uint4* const vcodes = reinterpret_cast<const uint4*>(cv.vcodes) + (size_t)kv * K;
+    const float *const kcoeffs = cv.kcoeffs + (size_t)kv * K, *const vcoeffs = cv.vcoeffs + (size_t)kv * K;
+    auto issue = [&](Stage<K>& st, int slot) {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             const int idx = i * 32 + lane, token = idx / K, plane = idx % K;
-            const long long s = __shfl_sync(0xffffffffu, slot, token);
-            const size_t from = s < 0 ? 0 : (size_t)s * step + plane;
-            copy_async<16>(&st.k[place<K>(token, plane)], kc + from, s >= 0);
-            copy_async<16>(&st.v[place<K>(token, plane)], vc + from, s >= 0);
+            const int s = __shfl_sync(0xffffffffu, slot, token);
+            const size_t from = (size_t)max(s, 0) * step + plane;
+            copy_async<16>(&st.k[place<K>(token, plane)], kcodes + from, s >= 0);
+            copy_async<16>(&st.v[place<K>(token, plane)], vcodes + from, s >= 0);
         }
-        const size_t from = (slot < 0 ? 0 : (size_t)slot * step) + (size_t)kv * K;
+        const size_t from = (size_t)max(slot, 0) * step;
         float *ka = st.ka + lane * pitch(K), *va = st.va + lane * pitch(K);
         constexpr int UNIT = K == 3 ? 1 : K;
         if (p.wide) {
 #pragma unroll
             for (int i = 0; i < K; i += UNIT) {
-                copy_async<4 * UNIT>(ka + i, cv.kcoeffs + from + i, slot >= 0);
-                copy_async<4 * UNIT>(va + i, cv.vcoeffs + from + i, slot >= 0);
+                copy_async<4 * UNIT>(ka + i, kcoeffs + from + i, slot >= 0);
+                copy_async<4 * UNIT>(va + i, vcoeffs + from + i, slot >= 0);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                copy_async<4>(ka + i, cv.kcoeffs + from + i, slot >= 0);
-                copy_async<4>(va + i, cv.vcoeffs + from + i, slot >= 0);
+                copy_async<4>(ka + i, kcoeffs + from + i, slot >= 0);
+                copy_async<4>(va + i, vcoeffs + from + i, slot >= 0);
             }
         }
     };
@@ -181,10 +205,10 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 
     int tile = tile0 + warp;
     uint32_t real[STAGES];              // tokens on a page, per stage
-    long long slot = slot_at(tile);
+    int slot = slot_at(tile);
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
-        const long long now = slot;
+        const int now = slot;
         slot = slot_at(tile + (s + 1) * WARPS);
         real[s] = __ballot_sync(0xffffffffu, now >= 0);
         if (real[s]) issue(stages[s], now);
@@ -234,17 +258,23 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
     }
     const float w0 = upper ? 16777216.0f : 65536.0f, w1 = upper ? 256.0f : 1.0f;        // digits' weights: keys
     const float wv = upper ? 65536.0f : 256.0f;                                         // values (row g + 8: 1 or nothing)
+    const f32x2 w0_2 = pack2(w0, w0), w1_2 = pack2(w1, w1), wv_2 = pack2(wv, wv);
+    const f32x2 minus_half0 = pack2(-half_sum[0], -half_sum[0]), minus_half1 = pack2(-half_sum[1], -half_sum[1]);
     const uint32_t sel = upper ? 0x62u : 0x51u, keep = upper ? 0xffffffffu : 0u;
     const uint32_t half = g & 1 ? 0x7362u : 0x5140u;        // bytes of the plane words that hold dimensions 16 g ..
-
-    float m = -INFINITY, l = 0.0f, o[16][2];
+    int start[4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) o[j][0] = o[j][1] = 0.0f;
+    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, 0x4B400000;" : "=r"(start[i]));
+
+    float m = -INFINITY, l = 0.0f;
+    f32x2 o[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] = pack2(0.0f, 0.0f);
 
     int stage = 0;
     for (; tile < tile1; tile += WARPS) {
         {
-            const long long now = slot;
+            const int now = slot;
             slot = slot_at(tile + STAGES * WARPS);
             real[STAGES - 1] = __ballot_sync(0xffffffffu, now >= 0);
             __syncwarp();
@@ -259,38 +289,67 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         for (int q = 0; q < STAGES - 1; ++q) real[q] = real[q + 1];
         stage = stage + 1 == STAGES ? 0 : stage + 1;
         if (on_a_page == 0) continue;           // (nothing was copied)
-        // tokens that this lane's row sees, from token 2 c on
+        // tokens that this lane's row sees
         const int left = my_limit - tile * TILE;
-        const uint32_t mask = (on_a_page & (left >= TILE ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u)) >> (2 * c);
+        const uint32_t seen = on_a_page & (left >= TILE ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u);
+
+        // The coefficients by planes, so that those of tokens 2 c, 2 c + 1 lie together; the values' largest decides the fixed point of the tile's
+        // weights.  (What lanes read of the last tile they have read: the shuffles of its maximum lie behind.)
+        uint32_t largest = 0;
+        float va[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            coef.k[i][lane] = st.ka[lane * pitch(K) + i];
+            va[i] = st.va[lane * pitch(K) + i];
+            largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
+        }
+        largest = __reduce_max_sync(0xffffffffu, largest);
+        if (largest >= 0x7f800000u) {           // NaN or infinite coefficients: they count for the rows that see them, and for those only
+            bool bad = false;
+            largest = 0;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                if (!isfinite(va[i])) { bad = true; va[i] = 0.0f; }
+                largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
+            }
+            largest = __reduce_max_sync(0xffffffffu, largest);
+            if (__ballot_sync(0xffffffffu, bad) & seen) l = NAN;
+        }
+#pragma unroll
+        for (int i = 0; i < K; ++i) coef.v[i][lane] = va[i];
+        __syncwarp();
+        const int ev = max((int)(largest >> 23), 22);
+        const float to_fixed = __int_as_float((275 - ev) << 23), from_fixed = __int_as_float((ev - 21) << 23);
 
         // scores of tokens 8 n + 2 c, 8 n + 2 c + 1
         float s[4][2];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            int acc[K][4];
+            f32x2 x = 0, y = 0, all = 0;
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = MAGIC_BITS;
+                int acc[4];
                 const uint32_t w = reinterpret_cast<const uint32_t*>(&st.k[place<K>(8 * n + g, i)])[c];
+                mma_s8u8(acc, aq[0], w & 0x01010101u, w & 0x02020202u, start);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mma_s8u8(acc[i], aq[j], w & (0x01010101u << (2 * j)), w & (0x02020202u << (2 * j)));
+                for (int j = 1; j < 4; ++j) mma_s8u8(acc, aq[j], w & (0x01010101u << (2 * j)), w & (0x02020202u << (2 * j)));
+                const f32x2 a = *reinterpret_cast<const f32x2*>(&coef.k[i][8 * n + 2 * c]);
+                x = i ? fma2(a, sums2(acc[0], acc[1]), x) : mul2(a, sums2(acc[0], acc[1]));
+                y = i ? fma2(a, sums2(acc[2], acc[3]), y) : mul2(a, sums2(acc[2], acc[3]));
+                all = i ? add2(all, a) : a;
             }
+            x = fma2(minus_half0, all, x);
+            y = fma2(minus_half1, all, y);
+            unpack2(fma2(w0_2, x, mul2(w1_2, y)), s[n][0], s[n][1]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float* a = st.ka + (8 * n + 2 * c + e) * pitch(K);
-                float x = 0.0f, y = 0.0f, all = 0.0f;
+            for (int e = 0; e < 2; ++e) s[n][e] = (s[n][e] + __shfl_xor_sync(0xffffffffu, s[n][e], 16)) * factor;
+        }
+        if (__any_sync(0xffffffffu, seen != 0xffffffffu)) {
+            const uint32_t mine = seen >> (2 * c);
 #pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    x = fmaf(a[i], __int_as_float(acc[i][e]) - MAGIC, x);
-                    y = fmaf(a[i], __int_as_float(acc[i][2 + e]) - MAGIC, y);
-                    all += a[i];
-                }
-                x = fmaf(-half_sum[0], all, x);
-                y = fmaf(-half_sum[1], all, y);
-                float v = fmaf(w0, x, w1 * y);
-                v += __shfl_xor_sync(0xffffffffu, v, 16);
-                s[n][e] = mask >> (8 * n + e) & 1 ? v * factor : -INFINITY;
-            }
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) s[n][e] = mine >> (8 * n + e) & 1 ? s[n][e] : -INFINITY;
         }
         // weights, relative to the tile's maximum
         float top = s[0][0];
@@ -301,80 +360,64 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         const float ref = top == -INFINITY ? 0.0f : top, m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.0f : m_new;
         const float corr = exp2_approx(m - m_ref), tile_factor = exp2_approx(top - m_ref);
         m = m_new;
-        // the values' coefficients: the largest decides the fixed point
-        float va[4][2][K];
-        uint32_t largest = 0;
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    va[n][e][i] = st.va[(8 * n + 2 * c + e) * pitch(K) + i];
-                    largest = max(largest, __float_as_uint(va[n][e][i]) & 0x7fffffffu);
-                }
-        largest = __reduce_max_sync(0xffffffffu, largest);
-        if (largest >= 0x7f800000u) {           // NaN or infinite coefficients: nobody's but the rows' that see them
-            largest = 0;
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int i = 0; i < K; ++i) {
-                        if (!isfinite(va[n][e][i])) {
-                            if (mask >> (8 * n + e) & 1) l = NAN;
-                            va[n][e][i] = 0.0f;
-                        }
-                        largest = max(largest, __float_as_uint(va[n][e][i]) & 0x7fffffffu);
-                    }
-            largest = __reduce_max_sync(0xffffffffu, largest);
-        }
-        const int ev = max((int)(largest >> 23), 22);
-        const float to_fixed = __int_as_float((275 - ev) << 23), from_fixed = __int_as_float((ev - 21) << 23);
         float sum = 0.0f;
         // weights times coefficients as digits: an MMA's 32 positions are 32 / pitch tokens, 8 / pitch of them this lane's
-        constexpr int PK = pitch(K), STEPS = PK, PER = 4 / PK;          // MMA steps of a tile; tokens in a register of four bytes
-        uint32_t ap[STEPS][4], bv[STEPS][2][2];
+        constexpr int PK = pitch(K);            // MMA steps of a tile
+        uint32_t ap[PK][4], bv[PK][2][2];
+        uint32_t y[8][PK], word[8][PK];         // by this lane's tokens, (n, e) = (0, 0), (0, 1), (1, 0), ..
 #pragma unroll
-        for (int z = 0; z < STEPS; ++z)
+        for (int n = 0; n < 4; ++n) {
+            const float e0 = exp2_approx(s[n][0] - ref), e1 = exp2_approx(s[n][1] - ref);
+            sum += e0 + e1;
+            const f32x2 ws = mul2(pack2(e0, e1), pack2(to_fixed, to_fixed));
+#pragma unroll
+            for (int i = 0; i < PK; ++i) {
+                if (i >= K) { y[2 * n][i] = y[2 * n + 1][i] = 0x00808080u; word[2 * n][i] = word[2 * n + 1][i] = 0u; continue; }
+                const int j = i < K ? i : 0;
+                float f0, f1;
+                unpack2(fma2(ws, *reinterpret_cast<const f32x2*>(&coef.v[j][8 * n + 2 * c]), pack2(MAGIC, MAGIC)), f0, f1);
+                y[2 * n][i] = (uint32_t)__float_as_int(f0) + (0x00808080u - (uint32_t)MAGIC_BITS);
+                y[2 * n + 1][i] = (uint32_t)__float_as_int(f1) + (0x00808080u - (uint32_t)MAGIC_BITS);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    word[2 * n + e][i] = reinterpret_cast<const uint32_t*>(&st.v[place<K>(8 * n + 2 * c + e, j)])[g >> 1];
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < PK; ++z)
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
-                uint32_t y[4], word[4];
+                uint32_t yy[4], ww[4];
 #pragma unroll
-                for (int u = 0; u < PER; ++u) {
-                    // this lane's tokens in order: (n, e) = (0, 0), (0, 1), (1, 0), ..
-                    const int q = (2 * z + side) * PER + u, n = q >> 1, e = q & 1;
-                    const float w = exp2_approx(s[n][e] - ref);
-                    sum += w;
-                    const float ws = w * to_fixed;
-#pragma unroll
-                    for (int i = 0; i < PK; ++i) {
-                        y[u * PK + i] = i < K ? (uint32_t)__float_as_int(fmaf(ws, va[n][e][i < K ? i : 0], MAGIC)) + (0x00808080u - (uint32_t)MAGIC_BITS) : 0x00808080u;
-                        word[u * PK + i] = i < K ? reinterpret_cast<const uint32_t*>(&st.v[place<K>(8 * n + 2 * c + e, i < K ? i : 0)])[g >> 1] : 0u;
-                    }
+                for (int u = 0; u < 4; ++u) {
+                    yy[u] = y[(2 * z + side) * (4 / PK) + u / PK][u % PK];
+                    ww[u] = word[(2 * z + side) * (4 / PK) + u / PK][u % PK];
                 }
-                ap[z][2 * side] = __byte_perm(__byte_perm(y[0], y[1], sel), __byte_perm(y[2], y[3], sel), 0x5410) ^ 0x80808080u;
-                ap[z][2 * side + 1] = (__byte_perm(__byte_perm(y[0], y[1], 0x40), __byte_perm(y[2], y[3], 0x40), 0x5410) ^ 0x80808080u) & keep;
-                const uint32_t t0 = __byte_perm(word[0], word[1], half), t1 = __byte_perm(word[2], word[3], half);
+                ap[z][2 * side] = __byte_perm(__byte_perm(yy[0], yy[1], sel), __byte_perm(yy[2], yy[3], sel), 0x5410) ^ 0x80808080u;
+                ap[z][2 * side + 1] = (__byte_perm(__byte_perm(yy[0], yy[1], 0x40), __byte_perm(yy[2], yy[3], 0x40), 0x5410) ^ 0x80808080u) & keep;
+                const uint32_t t0 = __byte_perm(ww[0], ww[1], half), t1 = __byte_perm(ww[2], ww[3], half);
                 bv[z][side][0] = __byte_perm(t0, t1, 0x5410);
                 bv[z][side][1] = __byte_perm(t0, t1, 0x7632);
             }
         l = fmaf(l, corr, sum * tile_factor);
-        int ones[4] = {MAGIC_BITS, MAGIC_BITS, MAGIC_BITS, MAGIC_BITS};
+        int ones[4];
+        mma_s8u8(ones, ap[0], 0x01010101u, 0x01010101u, start);
 #pragma unroll
-        for (int z = 0; z < STEPS; ++z) mma_s8u8(ones, ap[z], 0x01010101u, 0x01010101u);
+        for (int z = 1; z < PK; ++z) mma_s8u8(ones, ap[z], 0x01010101u, 0x01010101u);
         const float unit = tile_factor * from_fixed;
         const float base = -unit * fmaf(wv, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
+        const f32x2 base_2 = pack2(base, base), corr_2 = pack2(corr, corr);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            int acc[4] = {MAGIC_BITS, MAGIC_BITS, MAGIC_BITS, MAGIC_BITS};
+        for (int j = 0; j < 8; ++j) {
+            const f32x2 f = pack2(unit * (2.0f / (1 << j)), unit * (2.0f / (1 << j)));
 #pragma unroll
-            for (int z = 0; z < STEPS; ++z) mma_s8u8(acc, ap[z], bv[z][0][j >> 3] & (0x01010101u << (j & 7)), bv[z][1][j >> 3] & (0x01010101u << (j & 7)));
-            const float f = unit * (2.0f / (1 << (j & 7)));
+            for (int h = 0; h < 2; ++h) {
+                int acc[4];
+                mma_s8u8(acc, ap[0], bv[0][0][h] & (0x01010101u << j), bv[0][1][h] & (0x01010101u << j), start);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                o[j][e] = fmaf(fmaf(wv, __int_as_float(acc[e]) - MAGIC, __int_as_float(acc[2 + e]) - MAGIC), f, fmaf(o[j][e], corr, base));
+                for (int z = 1; z < PK; ++z) mma_s8u8(acc, ap[z], bv[z][0][h] & (0x01010101u << j), bv[z][1][h] & (0x01010101u << j));
+                o[8 * h + j] = fma2(fma2(wv_2, sums2(acc[0], acc[1]), sums2(acc[2], acc[3])), f, fma2(o[8 * h + j], corr_2, base_2));
+            }
         }
     }
 
@@ -385,12 +428,13 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
     __syncthreads();
     float (*s_o)[ROWS][AMQ_MAX_HEAD_DIM] = reinterpret_cast<float (*)[ROWS][AMQ_MAX_HEAD_DIM]>(smem_raw);
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float v = o[j][e] + __shfl_xor_sync(0xffffffffu, o[j][e], 16);
-            if (upper) s_o[warp][r][32 * c + 16 * e + j] = v;
-        }
+    for (int j = 0; j < 16; ++j) {
+        float v0, v1;
+        unpack2(o[j], v0, v1);
+        v0 += __shfl_xor_sync(0xffffffffu, v0, 16);
+        v1 += __shfl_xor_sync(0xffffffffu, v1, 16);
+        if (upper) { s_o[warp][r][32 * c + j] = v0; s_o[warp][r][32 * c + 16 + j] = v1; }
+    }
     if (lane < 16 && c == 0) { s_m[warp][r] = m; s_l[warp][r] = l; }
     __syncthreads();
 #pragma unroll
@@ -458,8 +502,8 @@ AttentionPlan attention_plan(int batch, int q_len, int q_heads, int heads, long 
 template <int K>
 amq_status launch_attention(const AttentionParams& p, unsigned grid, cudaStream_t st)
 {
-    const size_t smem = sizeof(Stage<K>) * STAGES * WARPS > sizeof(float) * WARPS * ROWS * AMQ_MAX_HEAD_DIM ? sizeof(Stage<K>) * STAGES * WARPS
-                                                                                                       : sizeof(float) * WARPS * ROWS * AMQ_MAX_HEAD_DIM;
+    constexpr size_t smem = WARPS * (sizeof(Stage<K>) * STAGES + sizeof(Coefficients<K>));
+    static_assert(smem >= sizeof(float) * WARPS * ROWS * AMQ_MAX_HEAD_DIM, "the partial sums take the stages' place");
     AMQ_CUDA_TRY(cudaFuncSetAttribute(cache_attention_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     AMQ_CUDA_TRY(launch_kernel(cache_attention_kernel<K>, dim3(grid), dim3(WARPS * 32), smem, st, true, p));
     AMQ_LAUNCH_CHECK();
@@ -471,8 +515,10 @@ amq_status cache_view(const uint32_t* kcodes, const float* kcoeffs, const uint32
 {
     if (pages < 0 || page_size < 1 || heads < 1 || d < 1 || max_pages < 0 || ld_table < max_pages) return AMQ_ERR_INVALID_ARG;
     if (!valid_k(k) || d > AMQ_MAX_HEAD_DIM || heads > 65535) return AMQ_ERR_UNSUPPORTED;
-    if ((long long)max_pages * page_size > AMQ_MAX_TOKENS) return AMQ_ERR_UNSUPPORTED;
-    *out = {kcodes, kcoeffs, vcodes, vcoeffs, pages, page_size, heads, d, k, words_per_row(d), table, ld_table, max_pages, lengths};
+    if ((long long)max_pages * page_size > AMQ_MAX_TOKENS || (long long)pages * page_size > AMQ_MAX_TOKENS) return AMQ_ERR_UNSUPPORTED;
+    int shift = -1;
+    for (int i = 0; i < 31; ++i) if (page_size == 1 << i) shift = i;
+    *out = {kcodes, kcoeffs, vcodes, vcoeffs, pages, page_size, shift, heads, d, k, words_per_row(d), table, ld_table, max_pages, lengths};
     return AMQ_OK;
 }
 
