@@ -2,6 +2,8 @@
 //
 //   s[t] = scale * sum_i a[t][i] (q . b[t][i]),   p = softmax over the visible t,   o = sum_t p[t] sum_i a'[t][i] b'[t][i]
 // with the planes b, b' (+-1) and coefficients a, a' of token t's key and value.
+#include <stddef.h>
+
 #include "amq_common.cuh"
 #include "amq_pairs.cuh"
 
@@ -100,12 +102,21 @@ template <int K> __device__ __forceinline__ int place(int token, int plane)
     return token;
 }
 
-template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from, bool real)
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* from, bool real)
 {
-    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
     const int n = real ? BYTES : 0;                 // (nothing is read for the others: zeros are written)
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(from), "r"(n) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" :: "r"(dst), "l"(from), "r"(n), "n"(BYTES) : "memory");
+}
+
+// a token's coefficients from shared memory, at once
+template <int K> __device__ __forceinline__ void load_row(const float* from, float (&v)[K])
+{
+    if constexpr (K == 4) { const float4 a = *reinterpret_cast<const float4*>(from); v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; }
+    else if constexpr (K == 2) { const float2 a = *reinterpret_cast<const float2*>(from); v[0] = a.x; v[1] = a.y; }
+    else
+#pragma unroll
+        for (int i = 0; i < K; ++i) v[i] = from[i];
 }
 
 __device__ __forceinline__ void mma_s8u8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -125,7 +136,7 @@ __device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint32_t (&a)[4], ui
 // two sums as floats: integers of up to 22 bits on top of MAGIC
 __device__ __forceinline__ f32x2 sums2(int a, int b) { return add2(pack2(__int_as_float(a), __int_as_float(b)), pack2(-MAGIC, -MAGIC)); }
 
-__device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 // The products run on the integer tensor cores, on the planes' bits as they are stored: a word ANDed with 0x01010101 << j is four bytes of 0 or
 // 2^j, an operand of mma.m16n8k32 with the query (or the weights) as digits of eight bits.  A query row is four rows of the operand, its
@@ -146,10 +157,15 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ float s_m[WARPS][ROWS], s_l[WARPS][ROWS];
+    __shared__ uint32_t s_largest[WARPS][ROWS];
+    __shared__ uint4 s_digits[WARPS][32];
+    __shared__ int s_sum[WARPS][8][2];
     const CacheView& cv = p.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3, r = g & 3;
-    const bool upper = g < 4;           // rows g, g + 8: digits 3 and 1 of the query (weights: 2 and 0), else 2 and 0 (1 and none)
+    const bool upper = g < 4;           // rows g, g + 8: digits 3 and 1, else 2 and 0
+    const uint32_t digit0 = upper ? 0x73u : 0x62u, digit1 = upper ? 0x51u : 0x40u;      // these bytes of two words
     Stage<K>* stages = reinterpret_cast<Stage<K>*>(smem_raw) + warp * STAGES;
+    const uint32_t stage_at = (uint32_t)__cvta_generic_to_shared(stages);
     Coefficients<K>& coef = (reinterpret_cast<Coefficients<K>*>(reinterpret_cast<Stage<K>*>(smem_raw) + WARPS * STAGES))[warp];
 
     int at = blockIdx.x;
@@ -171,33 +187,35 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         return tile < tile1 && t < limit ? slot_of(cv, b, t) : -1;
     };
     // planes: K lanes a token, so that an instruction's lanes meet few lines; coefficients: a lane a token
-    const size_t step = (size_t)cv.heads * K;
-    const uint4* const kcodes = reinterpret_cast<const uint4*>(cv.kcodes) + (size_t)kv * K;
-    const uint4* const vcodes = reinterpret_cast<const uint4*>(cv.vcodes) + (size_t)kv * K;
-    const float *const kcoeffs = cv.kcoeffs + (size_t)kv * K, *const vcoeffs = cv.vcoeffs + (size_t)kv * K;
-    auto issue = [&](Stage<K>& st, int slot) {
+    const uint32_t step = (uint32_t)cv.heads * K;           // planes of a token (at most 2^18)
+    const char* const kcodes = reinterpret_cast<const char*>(cv.kcodes) + (size_t)kv * K * 16;
+    const char* const vcodes = reinterpret_cast<const char*>(cv.vcodes) + (size_t)kv * K * 16;
+    const char* const kcoeffs = reinterpret_cast<const char*>(cv.kcoeffs + (size_t)kv * K);
+    const char* const vcoeffs = reinterpret_cast<const char*>(cv.vcoeffs + (size_t)kv * K);
+    auto issue = [&](uint32_t st, int slot) {               // st: address of the stage
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             const int idx = i * 32 + lane, token = idx / K, plane = idx % K;
             const int s = __shfl_sync(0xffffffffu, slot, token);
-            const size_t from = (size_t)max(s, 0) * step + plane;
-            copy_async<16>(&st.k[place<K>(token, plane)], kcodes + from, s >= 0);
-            copy_async<16>(&st.v[place<K>(token, plane)], vcodes + from, s >= 0);
+            const uint64_t from = (uint64_t)(uint32_t)max(s, 0) * (step * 16u);
+            const uint32_t to = st + place<K>(token, plane) * 16;
+            copy_async<16>(to, kcodes + plane * 16 + from, s >= 0);
+            copy_async<16>(to + (uint32_t)offsetof(Stage<K>, v), vcodes + plane * 16 + from, s >= 0);
         }
-        const size_t from = (size_t)max(slot, 0) * step;
-        float *ka = st.ka + lane * pitch(K), *va = st.va + lane * pitch(K);
+        const uint64_t from = (uint64_t)(uint32_t)max(slot, 0) * (step * 4u);
+        const uint32_t ka = st + (uint32_t)offsetof(Stage<K>, ka) + lane * pitch(K) * 4, va = st + (uint32_t)offsetof(Stage<K>, va) + lane * pitch(K) * 4;
         constexpr int UNIT = K == 3 ? 1 : K;
         if (p.wide) {
 #pragma unroll
             for (int i = 0; i < K; i += UNIT) {
-                copy_async<4 * UNIT>(ka + i, kcoeffs + from + i, slot >= 0);
-                copy_async<4 * UNIT>(va + i, vcoeffs + from + i, slot >= 0);
+                copy_async<4 * UNIT>(ka + 4 * i, kcoeffs + 4 * i + from, slot >= 0);
+                copy_async<4 * UNIT>(va + 4 * i, vcoeffs + 4 * i + from, slot >= 0);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                copy_async<4>(ka + i, kcoeffs + from + i, slot >= 0);
-                copy_async<4>(va + i, vcoeffs + from + i, slot >= 0);
+                copy_async<4>(ka + 4 * i, kcoeffs + 4 * i + from, slot >= 0);
+                copy_async<4>(va + 4 * i, vcoeffs + 4 * i + from, slot >= 0);
             }
         }
     };
@@ -211,66 +229,85 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         const int now = slot;
         slot = slot_at(tile + (s + 1) * WARPS);
         real[s] = __ballot_sync(0xffffffffu, now >= 0);
-        if (real[s]) issue(stages[s], now);
+        if (real[s]) issue(stage_at + s * (uint32_t)sizeof(Stage<K>), now);
         commit();
     }
 
-    // the query's digits as the MMAs take them, and the digits' sums (times the bytes' weights) over the row
+    // The query's digits as the MMAs take them, and the digits' sums (times the bytes' weights) over the row.  A warp makes those of two bit positions.
     uint32_t aq[4][4];
     float half_sum[2], factor;
     {
-        float x[32];
+        float x[8];
         uint32_t largest = 0;
-        const int i = row / p.group, h = kv * p.group + row % p.group;
-        const float* q = p.q + b * p.q_batch + i * p.q_token + h * p.q_head + 32 * c;
+        const int i = row / p.group, h = kv * p.group + row % p.group, first = 32 * c + 2 * warp;
+        const float* q = p.q + b * p.q_batch + i * p.q_token + h * p.q_head + first;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            x[j] = row < p.rows && 32 * c + j < cv.d ? q[j] : 0.0f;
-            largest = max(largest, __float_as_uint(x[j]) & 0x7fffffffu);
-        }
+        for (int byte = 0; byte < 4; ++byte)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                x[2 * byte + j] = row < p.rows && first + 8 * byte + j < cv.d ? q[8 * byte + j] : 0.0f;
+                largest = max(largest, __float_as_uint(x[2 * byte + j]) & 0x7fffffffu);
+            }
         largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
         largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
+        if (upper && c == 0) s_largest[warp][r] = largest;
+        __syncthreads();
+        largest = max(max(s_largest[0][r], s_largest[1][r]), max(s_largest[2][r], s_largest[3][r]));
         const int e = max((int)(largest >> 23), 29);
         const bool finite = largest < 0x7f800000u;
         const float to_fixed = finite ? __int_as_float((283 - e) << 23) : 0.0f;         // largest element below 2^30
+        const float to_fixed_here = to_fixed * __int_as_float((127 - 2 * warp) << 23);
         int sum[2] = {0, 0};
+        uint32_t a[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t a0 = 0, a1 = 0;
+        for (int j = 0; j < 2; ++j) {
+            uint32_t y[4];
 #pragma unroll
             for (int byte = 0; byte < 4; ++byte) {
-                const uint32_t y = (uint32_t)__float2int_rn(x[j + 8 * byte] * to_fixed * (1.0f / (1 << j))) + 0x80808080u;
-                const int d0 = (int)((upper ? y >> 24 : y >> 16) & 255u) - 128, d1 = (int)((upper ? y >> 8 : y) & 255u) - 128;
-                a0 |= (uint32_t)(d0 & 255) << (8 * byte);
-                a1 |= (uint32_t)(d1 & 255) << (8 * byte);
-                sum[0] += d0 * (1 << j); sum[1] += d1 * (1 << j);
+                y[byte] = (uint32_t)__float2int_rn(x[2 * byte + j] * to_fixed_here * (j ? 0.5f : 1.0f)) + 0x80808080u;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) sum[w] += ((int)(__byte_perm(y[byte], 0, w ? digit1 & 0x7u : digit0 & 0x7u) & 255u) - 128) * (1 << j);
             }
-            aq[j >> 1][(j & 1) * 2] = a0;
-            aq[j >> 1][(j & 1) * 2 + 1] = a1;
+            a[2 * j] = __byte_perm(__byte_perm(y[0], y[1], digit0), __byte_perm(y[2], y[3], digit0), 0x5410) ^ 0x80808080u;
+            a[2 * j + 1] = __byte_perm(__byte_perm(y[0], y[1], digit1), __byte_perm(y[2], y[3], digit1), 0x5410) ^ 0x80808080u;
         }
+        s_digits[warp][lane] = make_uint4(a[0], a[1], a[2], a[3]);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], 1);
             sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], 2);
-            half_sum[w] = 0.5f * (float)sum[w];
+            if (c == 0) s_sum[warp][g][w] = sum[w] * (1 << (2 * warp));
         }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint4 d = s_digits[j][lane];
+            aq[j][0] = d.x; aq[j][1] = d.y; aq[j][2] = d.z; aq[j][3] = d.w;
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) half_sum[w] = 0.5f * (float)(s_sum[0][g][w] + s_sum[1][g][w] + s_sum[2][g][w] + s_sum[3][g][w]);
         factor = finite ? 1.0f / to_fixed * p.scale * (2.0f * 1.44269504f) : NAN;       // scores in units of log 2
     }
-    const float w0 = upper ? 16777216.0f : 65536.0f, w1 = upper ? 256.0f : 1.0f;        // digits' weights: keys
-    const float wv = upper ? 65536.0f : 256.0f;                                         // values (row g + 8: 1 or nothing)
-    const f32x2 w0_2 = pack2(w0, w0), w1_2 = pack2(w1, w1), wv_2 = pack2(wv, wv);
+    const float w0 = upper ? 16777216.0f : 65536.0f, w1 = upper ? 256.0f : 1.0f;        // the digits' weights
+    const f32x2 w0_2 = pack2(w0, w0), w1_2 = pack2(w1, w1);
     const f32x2 minus_half0 = pack2(-half_sum[0], -half_sum[0]), minus_half1 = pack2(-half_sum[1], -half_sum[1]);
-    const uint32_t sel = upper ? 0x62u : 0x51u, keep = upper ? 0xffffffffu : 0u;
     const uint32_t half = g & 1 ? 0x7362u : 0x5140u;        // bytes of the plane words that hold dimensions 16 g ..
     int start[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, 0x4B400000;" : "=r"(start[i]));
+    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, %1;" : "=r"(start[i]) : "n"(MAGIC_BITS));
 
     float m = -INFINITY, l = 0.0f;
     f32x2 o[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[j] = pack2(0.0f, 0.0f);
 
+    // this lane's words of a plane: of token g of eight (keys), of token 2 c (values; the next token's lie a pitch on)
+    uint32_t kat[K], vat[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        kat[i] = place<K>(g, i) * 16 + c * 4;
+        vat[i] = (uint32_t)offsetof(Stage<K>, v) + place<K>(2 * c, i) * 16 + (g >> 1) * 4;
+    }
     int stage = 0;
     for (; tile < tile1; tile += WARPS) {
         {
@@ -278,12 +315,13 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             slot = slot_at(tile + STAGES * WARPS);
             real[STAGES - 1] = __ballot_sync(0xffffffffu, now >= 0);
             __syncwarp();
-            if (real[STAGES - 1]) issue(stages[stage == 0 ? STAGES - 1 : stage - 1], now);
+            if (real[STAGES - 1]) issue(stage_at + (stage == 0 ? STAGES - 1 : stage - 1) * (uint32_t)sizeof(Stage<K>), now);
             commit();
             asm volatile("cp.async.wait_group %0;" :: "n"(STAGES - 1) : "memory");
             __syncwarp();
         }
         const Stage<K>& st = stages[stage];
+        const char* const words = reinterpret_cast<const char*>(&st);
         const uint32_t on_a_page = real[0];
 #pragma unroll
         for (int q = 0; q < STAGES - 1; ++q) real[q] = real[q + 1];
@@ -294,13 +332,15 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         const uint32_t seen = on_a_page & (left >= TILE ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u);
 
         // The coefficients by planes, so that those of tokens 2 c, 2 c + 1 lie together; the values' largest decides the fixed point of the tile's
-        // weights.  (What lanes read of the last tile they have read: the shuffles of its maximum lie behind.)
+        // weights.  (The barrier behind the copies lies behind everybody's reading of the last tile's.)
         uint32_t largest = 0;
         float va[K];
+        float ka[K];
+        load_row<K>(st.ka + lane * pitch(K), ka);
+        load_row<K>(st.va + lane * pitch(K), va);
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            coef.k[i][lane] = st.ka[lane * pitch(K) + i];
-            va[i] = st.va[lane * pitch(K) + i];
+            coef.k[i][lane] = ka[i];
             largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
         }
         largest = __reduce_max_sync(0xffffffffu, largest);
@@ -318,8 +358,8 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 #pragma unroll
         for (int i = 0; i < K; ++i) coef.v[i][lane] = va[i];
         __syncwarp();
-        const int ev = max((int)(largest >> 23), 22);
-        const float to_fixed = __int_as_float((275 - ev) << 23), from_fixed = __int_as_float((ev - 21) << 23);
+        const int ev = max((int)(largest >> 23), 30);
+        const float to_fixed = __int_as_float((283 - ev) << 23), from_fixed = __int_as_float((ev - 29) << 23);       // products below 2^30
 
         // scores of tokens 8 n + 2 c, 8 n + 2 c + 1
         float s[4][2];
@@ -329,7 +369,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 #pragma unroll
             for (int i = 0; i < K; ++i) {
                 int acc[4];
-                const uint32_t w = reinterpret_cast<const uint32_t*>(&st.k[place<K>(8 * n + g, i)])[c];
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(words + kat[i] + n * 8 * pitch(K) * 16);
                 mma_s8u8(acc, aq[0], w & 0x01010101u, w & 0x02020202u, start);
 #pragma unroll
                 for (int j = 1; j < 4; ++j) mma_s8u8(acc, aq[j], w & (0x01010101u << (2 * j)), w & (0x02020202u << (2 * j)));
@@ -372,15 +412,15 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             const f32x2 ws = mul2(pack2(e0, e1), pack2(to_fixed, to_fixed));
 #pragma unroll
             for (int i = 0; i < PK; ++i) {
-                if (i >= K) { y[2 * n][i] = y[2 * n + 1][i] = 0x00808080u; word[2 * n][i] = word[2 * n + 1][i] = 0u; continue; }
+                if (i >= K) { y[2 * n][i] = y[2 * n + 1][i] = 0x80808080u; word[2 * n][i] = word[2 * n + 1][i] = 0u; continue; }
                 const int j = i < K ? i : 0;
                 float f0, f1;
-                unpack2(fma2(ws, *reinterpret_cast<const f32x2*>(&coef.v[j][8 * n + 2 * c]), pack2(MAGIC, MAGIC)), f0, f1);
-                y[2 * n][i] = (uint32_t)__float_as_int(f0) + (0x00808080u - (uint32_t)MAGIC_BITS);
-                y[2 * n + 1][i] = (uint32_t)__float_as_int(f1) + (0x00808080u - (uint32_t)MAGIC_BITS);
+                unpack2(mul2(ws, *reinterpret_cast<const f32x2*>(&coef.v[j][8 * n + 2 * c])), f0, f1);
+                y[2 * n][i] = (uint32_t)__float2int_rn(f0) + 0x80808080u;
+                y[2 * n + 1][i] = (uint32_t)__float2int_rn(f1) + 0x80808080u;
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    word[2 * n + e][i] = reinterpret_cast<const uint32_t*>(&st.v[place<K>(8 * n + 2 * c + e, j)])[g >> 1];
+                    word[2 * n + e][i] = *reinterpret_cast<const uint32_t*>(words + vat[j] + (n * 8 + e) * pitch(K) * 16);
             }
         }
 #pragma unroll
@@ -393,8 +433,8 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
                     yy[u] = y[(2 * z + side) * (4 / PK) + u / PK][u % PK];
                     ww[u] = word[(2 * z + side) * (4 / PK) + u / PK][u % PK];
                 }
-                ap[z][2 * side] = __byte_perm(__byte_perm(yy[0], yy[1], sel), __byte_perm(yy[2], yy[3], sel), 0x5410) ^ 0x80808080u;
-                ap[z][2 * side + 1] = (__byte_perm(__byte_perm(yy[0], yy[1], 0x40), __byte_perm(yy[2], yy[3], 0x40), 0x5410) ^ 0x80808080u) & keep;
+                ap[z][2 * side] = __byte_perm(__byte_perm(yy[0], yy[1], digit0), __byte_perm(yy[2], yy[3], digit0), 0x5410) ^ 0x80808080u;
+                ap[z][2 * side + 1] = __byte_perm(__byte_perm(yy[0], yy[1], digit1), __byte_perm(yy[2], yy[3], digit1), 0x5410) ^ 0x80808080u;
                 const uint32_t t0 = __byte_perm(ww[0], ww[1], half), t1 = __byte_perm(ww[2], ww[3], half);
                 bv[z][side][0] = __byte_perm(t0, t1, 0x5410);
                 bv[z][side][1] = __byte_perm(t0, t1, 0x7632);
@@ -404,8 +444,8 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         mma_s8u8(ones, ap[0], 0x01010101u, 0x01010101u, start);
 #pragma unroll
         for (int z = 1; z < PK; ++z) mma_s8u8(ones, ap[z], 0x01010101u, 0x01010101u);
-        const float unit = tile_factor * from_fixed;
-        const float base = -unit * fmaf(wv, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
+        const float unit = tile_factor * from_fixed * w1;           // (w0 = 2^16 w1)
+        const float base = -unit * fmaf(65536.0f, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
         const f32x2 base_2 = pack2(base, base), corr_2 = pack2(corr, corr);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -416,7 +456,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
                 mma_s8u8(acc, ap[0], bv[0][0][h] & (0x01010101u << j), bv[0][1][h] & (0x01010101u << j), start);
 #pragma unroll
                 for (int z = 1; z < PK; ++z) mma_s8u8(acc, ap[z], bv[z][0][h] & (0x01010101u << j), bv[z][1][h] & (0x01010101u << j));
-                o[8 * h + j] = fma2(fma2(wv_2, sums2(acc[0], acc[1]), sums2(acc[2], acc[3])), f, fma2(o[8 * h + j], corr_2, base_2));
+                o[8 * h + j] = fma2(fma2(pack2(65536.0f, 65536.0f), sums2(acc[0], acc[1]), sums2(acc[2], acc[3])), f, fma2(o[8 * h + j], corr_2, base_2));
             }
         }
     }
