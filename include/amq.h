@@ -342,7 +342,7 @@ AMQ_API amq_status amq_log_softmax_argmax(const float* logits, int rows, int n, 
  *   table   [batch][ld_table] int32, ld_table >= max_pages: the page of tokens [j * page_size, (j + 1) * page_size) of sequence b is
  *           table[b][j]; entries outside [0, pages) name none, and entries of pages that the length does not reach are not read.
  *   lengths [batch] int32: tokens of each sequence, the newest included; taken as at least 0 and at most max_pages * page_size by the attention.
- * 1 <= k <= 4; d up to AMQ_MAX_HEAD_DIM; max_pages * page_size up to AMQ_MAX_TOKENS; code pointers 16-byte aligned.
+ * 1 <= k <= 4; d up to AMQ_MAX_HEAD_DIM; max_pages * page_size and pages * page_size up to AMQ_MAX_TOKENS; code pointers 16-byte aligned.
  *
  * amq_cache_append: the rows of the `count` newest tokens of every sequence (kcodes [batch][count][heads][k][wpr(d)] and so on, 16-byte aligned
  * codes) go to positions lengths[b] - count .. lengths[b] - 1.  Rows whose position is negative, lies behind the table or on no page
@@ -365,8 +365,9 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  *   out [batch][q_len][q_heads][d] fp32.
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
  *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
- * Products with the planes are exact integers on q and p held as 22-bit fixed-point numbers (relative to a query's largest element, and
- * to the largest weight among 32 tokens); everything else is fp32.  Results repeat bit for bit for the same sizes.
+ * Products with the planes are exact, on q and on p times coefficients held as 31-bit fixed-point numbers (relative to a query's largest element, and
+ * to the largest weight and coefficient among 32 tokens; elements of a query below 2^-98 lose bits); everything else is fp32.  Results repeat
+ * bit for bit for the same sizes and lengths.
  */
 AMQ_API size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens);
 AMQ_API amq_status amq_cache_attention(const float* q, long long q_batch, long long q_token, long long q_head,

@@ -33,7 +33,7 @@ def values(amq, codes, coeffs, d):
 
 
 def expected(amq, q, cache, table, lengths, scale):
-    """(result, allowed error).  q enters as fixed-point numbers of 22 bits relative to a query's largest element and p to the largest of 32 tokens, so
+    """(result, allowed error).  q enters as fixed-point numbers of 23 bits or more relative to a query's largest element and p to the largest of 32 tokens, so
     a score is off by 2^-22 (and its fp32 roundings) of scale * sum_i |a_i| * d * max|q|, a weight by that and 2^-22; a weight's error counts twice
     (in the sum and in the normalisation)."""
     batch, q_len, q_heads, d = q.shape
