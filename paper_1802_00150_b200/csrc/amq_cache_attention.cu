@@ -116,6 +116,10 @@ __device__ __forceinline__ long long total_tiles(const AttentionParams& p)
     }
     return total;
 }
+// The shares that a line of so many tiles goes to: the lengths may be far below what the table has room for, and a share without tiles would leave nothing for the
+// second kernel to join.
+__device__ __forceinline__ int shares_of(const AttentionParams& p, long long total) { return (int)min((long long)p.shares, (total + 3) / 4); }
+
 // the sequence that holds place x of the line (x below the total), and the tiles in front of it
 __device__ __forceinline__ int sequence_at(const AttentionParams& p, long long x, long long* before)
 {
@@ -189,9 +193,10 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
     long long x = 0, x1 = 1, before = 0;
     if (p.shares) {
         const long long total = total_tiles(p);
-        x = total * share / p.shares;
-        x1 = total * (share + 1) / p.shares;
-        if (x >= x1) return;
+        const int shares = shares_of(p, total);
+        if (share >= shares) return;
+        x = total * share / shares;
+        x1 = total * (share + 1) / shares;
         b = sequence_at(p, x, &before);
     }
     tiles = tiles_of(cv, b);
@@ -639,10 +644,11 @@ cache_attention_join_kernel(const __grid_constant__ AttentionParams p, int block
         front += (long long)__reduce_add_sync(0xffffffffu, (uint32_t)n & 0xffffu) + ((long long)__reduce_add_sync(0xffffffffu, (uint32_t)n >> 16) << 16);
     }
     const long long total = total_tiles(p), x = front;
+    const int shares = shares_of(p, total);
     auto share_of = [&](long long at) {
-        long long s = at * p.shares / total;
-        while (total * (s + 1) / p.shares <= at) ++s;
-        while (total * s / p.shares > at) --s;
+        long long s = at * shares / total;
+        while (total * (s + 1) / shares <= at) ++s;
+        while (total * s / shares > at) --s;
         return (int)s;
     };
     int first = 0, last = 0;

@@ -83,6 +83,9 @@ CASES = [  # lengths, page size, heads, group, d, k, q_len
     ([1500, 1, 700], 1, 5, 3, 100, 3, 3), ([129, 1000], 64, 3, 8, 128, 4, 1), ([2, 5, 1, 0], 4, 2, 5, 127, 2, 4), ([4000], 16, 2, 4, 128, 4, 1),
     ([20000], 64, 1, 1, 128, 4, 1), ([9000], 7, 2, 8, 80, 2, 2), ([400, 399], 16, 16, 1, 128, 1, 1), ([260], 256, 2, 2, 33, 4, 6),
     ([40], 16, 1, 1, 128, 4, 40), ([70000], 64, 1, 8, 128, 3, 1), ([50] * 90, 16, 2, 4, 64, 4, 1), ([3000], 1000, 4, 4, 128, 2, 1),
+    # sequences without tokens between others, more than a warp of them; more blocks than CTAs fit the GPU
+    ([0, 0, 700, 0, 1, 0, 900] + [0] * 40 + [33, 0, 64] * 10 + [0, 5], 16, 2, 4, 64, 4, 1), ([600, 40], 16, 16, 4, 128, 2, 40),
+    ([0] * 70 + [2000], 32, 1, 8, 128, 1, 1), ([513] * 40, 1, 4, 1, 128, 4, 1),
 ]
 
 
@@ -202,6 +205,22 @@ def test_a_cache_beyond_32_bit_offsets(amq):
     amq.cache_append(rows[0], rows[1], rows[2], rows[3], cache, there, torch.tensor([200], dtype=torch.int32, device="cuda"), d)
     for big, row in zip(cache, rows):
         assert torch.equal(big[pages - 1, 199], row[0, 0])
+
+
+@pytest.mark.parametrize("k,group", [(1, 8), (4, 4), (2, 3)])
+@pytest.mark.parametrize("lengths", [[40, 0, 3], [1, 0, 0], [0, 0, 0], [130, 2000, 17], [2049, 1, 4096]])
+def test_a_table_with_room_for_more(amq, lengths, k, group):
+    """Lengths far below what the table has room for: fewer shares than CTAs, and no share without tokens."""
+    gen = torch.Generator(device="cuda").manual_seed(26)
+    small, pages = tables(gen, 3, [max(n, 1) for n in lengths], 16)
+    cache = filled(amq, gen, pages, 16, 2, 128, k)
+    table = torch.full((3, 512), -1, dtype=torch.int32, device="cuda")
+    table[:, :small.shape[1]] = small
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    q = torch.randn((3, 1, 2 * group, 128), device="cuda", generator=gen)
+    want = expected(amq, q, cache, table, n, 0.1)
+    ws = torch.full((amq.cache_attention_workspace_bytes(3, 1, 2 * group, 2, 128, 8192),), 255, dtype=torch.uint8, device="cuda")     # (NaN, should it be read)
+    close(amq.cache_attention(q, cache, table, n, 0.1, ws), want)
 
 
 def test_attention_in_a_graph_and_on_another_stream(amq):
