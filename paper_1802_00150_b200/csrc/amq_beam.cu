@@ -129,6 +129,7 @@ __global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(MAX_THREADS, 1)
 beam_select_kernel(SelectParams p)
 {
     constexpr int CHUNK = THREADS * PT, WARPS = THREADS / 32;
+    constexpr int SURE = PT <= 2 ? 0 : PT == 5 ? 2 : PT == 8 ? 5 : PT == 10 ? 8 : PT == 12 ? 10 : PT == 16 ? 12 : PT == 21 ? 16 : 21;      // (the size below)
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ float s_score[AMQ_MAX_BEAMS];
     __shared__ int s_done[AMQ_MAX_BEAMS];
@@ -156,6 +157,9 @@ beam_select_kernel(SelectParams p)
         if (lo + (c + 1) * CHUNK <= hi) {
 #pragma unroll
             for (int i = 0; i < PT; ++i) v[i] = __ldcg(z + i * THREADS);
+        } else if (lo + c * CHUNK + SURE * THREADS <= hi) {         // (a row's only piece, as a rule: its first words need no comparison)
+#pragma unroll
+            for (int i = 0; i < PT; ++i) v[i] = i < SURE || first + i * THREADS < hi ? __ldcg(z + i * THREADS) : -INFINITY;
         } else {
 #pragma unroll
             for (int i = 0; i < PT; ++i) v[i] = first + i * THREADS < hi ? __ldcg(z + i * THREADS) : -INFINITY;

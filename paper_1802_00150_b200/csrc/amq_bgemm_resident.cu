@@ -28,6 +28,9 @@ struct ResGemmParams {
 // Row stride of the results staged for the stores: 8 mod 32 words for two vectors (conflict-free in the m16n8 layout), 16-byte rows.
 constexpr int Y_LD = 132;
 constexpr int BIAS_BYTES = 2 * 128 * 4;     // POST: bias of a tile's rows, double-buffered
+// what lies behind the synchronisation block starts on 16 bytes, as the block does
+constexpr int SYNC_BYTES = ((int)sizeof(ResSync) + 15) / 16 * 16;
+static_assert(RES_TABLE * 4 % 16 == 0 && RES_ROW_BYTES % 16 == 0 && RES_ALPHA_BYTES % 16 == 0 && Y_LD * 4 % 16 == 0, "");
 // groups of eight vectors per epilogue thread: TB <= 64, or 32 (registers)
 __host__ __device__ constexpr int res_ng(int k_a) { return k_a <= 2 ? 2 : 1; }
 
@@ -49,7 +52,8 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
     uint32_t* table = reinterpret_cast<uint32_t*>(sAlpha + 2 * AMQ_MAX_K * 128);
     float* sY = reinterpret_cast<float*>(table + RES_TABLE);                        // [TB][Y_LD] results of a tile
     ResSync& sy = *reinterpret_cast<ResSync*>(sY + p.TB * Y_LD);
-    float* sBias = reinterpret_cast<float*>(&sy + 1);                               // POST: [2][128]
+    float* sBias = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(&sy) + SYNC_BYTES);    // POST: [2][128]
+    float* sR = sBias + 2 * 128;                                                    // POST, where there is a residual: [TB][Y_LD]
     const uint32_t sB = smem_u32(smem_raw);
 
     // this CTA's share of the (block, tile) list; a pass is the part of it that lies in one block of vectors
@@ -207,44 +211,40 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
                     if (row + 3 < p.units) out[3] = v.w;
                 }
             };
+            // The residual of a tile comes by asynchronous copies, a tile ahead, each lane's to where that lane will read it: a window of loads in registers left
+            // these three warps waiting (32768 x 1024, 512 vectors, residual alone: 85 us, 71 so).  It may be y itself: every element is read by the thread that
+            // writes it, before.
+            const int first = warp - R::MMA_WARP - 1;
+            auto fetch = [&](int t, int e) {
+                const int row = (tile0 + t) * 128 + 4 * lane;
+                const uint32_t to = smem_u32(sR + e * Y_LD + 4 * lane);
+                const float* from = a.residual + (size_t)(b0 + e) * a.ldr + row;
+                if (VEC && row + 3 < p.units) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+                } else {
+                    for (int q = 0; q < 4 && row + q < p.units; ++q)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(to + 4 * q), "l"(from + q) : "memory");
+                }
+            };
+            if (POST && a.residual)
+                for (int e = first; e < last; e += R::OUT_WARPS) fetch(0, e);
             for (int t = 0; t < tiles && ok; ++t) {
                 const int row = (tile0 + t) * 128 + 4 * lane;
                 const bool vec = VEC && row + 3 < p.units;
                 if constexpr (POST) {
-                    // The residual, a window of vectors ahead, of the next tile as far as L2: the stores may be over it (y = residual), so that the compiler
-                    // moves no load in front of one; every element is read by the thread that writes it, before.
-                    constexpr int WINDOW = 6;
-                    const int first = warp - R::MMA_WARP - 1;
-                    auto fetch = [&](int e) {
-                        float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (e >= last || !a.residual) return r;
-                        const float* res = a.residual + (size_t)(b0 + e) * a.ldr + row;
-                        if (vec) return __ldcg(reinterpret_cast<const float4*>(res));
-                        if (row < p.units) r.x = __ldcg(res);
-                        if (row + 1 < p.units) r.y = __ldcg(res + 1);
-                        if (row + 2 < p.units) r.z = __ldcg(res + 2);
-                        if (row + 3 < p.units) r.w = __ldcg(res + 3);
-                        return r;
-                    };
-                    float4 r[WINDOW];
-#pragma unroll
-                    for (int q = 0; q < WINDOW; ++q) r[q] = fetch(first + q * R::OUT_WARPS);
-                    if (a.residual && t + 1 < tiles && (lane & 7) == 0 && row + 128 < p.units)
-                        for (int e = first; e < last; e += R::OUT_WARPS)
-                            asm volatile("prefetch.global.L2 [%0];" :: "l"(a.residual + (size_t)(b0 + e) * a.ldr + row + 128));
                     ok = __all_sync(0xffffffffu, mbar_wait_relaxed(smem_u32(&sy.yfull), y_parity, &sy.failed));
                     y_parity ^= 1u;
                     if (!ok) { *(volatile int*)&sy.failed = 1; break; }
-                    for (int e0 = first; e0 < last; e0 += WINDOW * R::OUT_WARPS) {
-#pragma unroll
-                        for (int q = 0; q < WINDOW; ++q) {
-                            const int e = e0 + q * R::OUT_WARPS;
-                            if (e >= last) break;
-                            float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
-                            v.x += r[q].x; v.y += r[q].y; v.z += r[q].z; v.w += r[q].w;
-                            r[q] = fetch(e + WINDOW * R::OUT_WARPS);
-                            store(e, row, vec, v);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 4
+                    for (int e = first; e < last; e += R::OUT_WARPS) {
+                        float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
+                        if (a.residual) {
+                            const float4 r = *reinterpret_cast<const float4*>(sR + e * Y_LD + 4 * lane);
+                            v.x += r.x; v.y += r.y; v.z += r.z; v.w += r.w;
+                            if (t + 1 < tiles) fetch(t + 1, e);
                         }
+                        store(e, row, vec, v);
                     }
                     __syncwarp();
                     if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(&sy.yempty)) : "memory");
@@ -297,12 +297,13 @@ bool plan(const GemmArgs& g, int sms, ResGemmPlan* out)
     p.cell = RES_PLAIN; p.units = g.m;
     p.n = g.n; p.NS = (g.n + 255) / 256; p.batch = g.batch;
     a.mtiles = (g.m + 127) / 128;
+    auto post_bytes = [&](int TB) { return (size_t)TB * Y_LD * 4 * (g.post && g.residual ? 2 : 1) + (g.post ? BIAS_BYTES + 16 : 0); };
     // block of vectors: the size with the least estimated time (shares of tiles x steps, plus the expansion of the operand,
     // which a share pays at least once); sizes whose operand does not fit shared memory are out (n > 28000 or so: none fits)
     double best = 0.0;
     for (int TB = 8; TB <= 8 * res_ng(g.k_a) * R::SPLIT; TB += 8) {
         ResProblem q = p;
-        if (!res_set_block<R>(q, TB, g.k_a, (size_t)TB * Y_LD * 4 + (g.post ? BIAS_BYTES : 0))) break;
+        if (!res_set_block<R>(q, TB, g.k_a, post_bytes(TB))) break;
         const long long blocks = (g.batch + TB - 1) / TB, per_cta = (blocks * a.mtiles + sms - 1) / sms;
         const double expand = (double)q.N * q.NS * 128 / 80.0 + 1500.0;
         const double t = (double)per_cta * q.k_w * q.NS * res_slot_clocks(q) + expand * (1.0 + (double)per_cta / a.mtiles);
@@ -314,7 +315,7 @@ bool plan(const GemmArgs& g, int sms, ResGemmPlan* out)
     a.xcodes = g.xcodes; a.xbeta = g.xbeta; a.bias = g.bias; a.y = g.y; a.ldy = g.ldy;
     const long long total = (long long)a.blocks * a.mtiles;
     out->grid = (int)(total < sms ? total : sms);
-    out->smem = res_smem_bytes(a.p) + (size_t)a.p.TB * Y_LD * 4 + (g.post ? BIAS_BYTES : 0);
+    out->smem = res_smem_bytes(a.p) + post_bytes(a.p.TB);
     a.early_weights = !g.from_entry;
     a.activation = g.activation; a.residual = g.residual; a.ldr = g.ldr;
     out->vec_out = aligned16(g.y) && g.ldy % 4 == 0 && (!g.residual || (aligned16(g.residual) && g.ldr % 4 == 0));
