@@ -487,6 +487,10 @@ amq_status amq_beam_reorder(const void* const* src, void* const* dst, const size
         p.src[i] = static_cast<const char*>(src[i]); p.dst[i] = static_cast<char*>(dst[i]);
         p.src_stride[i] = (long long)src_stride[i]; p.dst_stride[i] = (long long)dst_stride[i];
     }
+    // a state that is written twice, or read by another one's threads while its own write it
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < count; ++j)
+            if (i != j && row_bytes[i] && row_bytes[j] && (dst[i] == dst[j] || dst[i] == src[j])) return AMQ_ERR_INVALID_ARG;
     long long most = 0;
     for (int i = 0; i < count; ++i) {
         p.columns[i] = (int)(row_bytes[i] / (wide ? 16 : 4));

@@ -36,9 +36,9 @@ cache_append_kernel(const __grid_constant__ AppendParams p)
     V coeff;
     if (codes) chunk = __ldcg((value ? p.vcodes : p.kcodes) + token * n + piece);
     else coeff = __ldcg(reinterpret_cast<const V*>(value ? p.vcoeffs : p.kcoeffs) + token * n + piece);
-    const int t = p.c.lengths[b] - p.count + i;
+    const long long t = (long long)p.c.lengths[b] - p.count + i;
     if (t < 0 || t >= (long long)p.c.max_pages * p.c.page_size) return;
-    const int slot = slot_of(p.c, b, t);
+    const int slot = slot_of(p.c, b, (int)t);
     if (slot < 0) return;
     if (codes) (value ? p.to_vcodes : p.to_kcodes)[(long long)slot * n + piece] = chunk;
     else reinterpret_cast<V*>(value ? p.to_vcoeffs : p.to_kcoeffs)[(long long)slot * n + piece] = coeff;

@@ -395,7 +395,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 
         // The coefficients by planes, so that those of tokens 2 c, 2 c + 1 lie together; the values' largest decides the fixed point of the tile's
         // weights.  (The barrier behind the copies lies behind everybody's reading of the last tile's.)
-        uint32_t largest = 0;
+        uint32_t largest = 0, largest_k = 0;
         float va[K];
         float ka[K];
         load_row<K>(st.ka + lane * pitch(K), ka);
@@ -404,10 +404,11 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         for (int i = 0; i < K; ++i) {
             coef.k[i][lane] = ka[i];
             largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
+            largest_k = max(largest_k, __float_as_uint(ka[i]) & 0x7fffffffu);
         }
-        largest = __reduce_max_sync(0xffffffffu, largest);
+        largest = __reduce_max_sync(0xffffffffu, largest_k >= 0x7f800000u ? largest_k : largest);
         if (largest >= 0x7f800000u) {           // NaN or infinite coefficients: they count for the rows that see them, and for those only
-            bool bad = false;
+            bool bad = largest_k >= 0x7f800000u;
             largest = 0;
 #pragma unroll
             for (int i = 0; i < K; ++i) {

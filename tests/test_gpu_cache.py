@@ -186,6 +186,24 @@ def test_nothing_hidden_counts(amq):
     assert torch.isnan(got[1, 0, 2:]).all() and not torch.isnan(got[1, 0, :2]).any() and not torch.isnan(got[0]).any() and not torch.isnan(got[2]).any()
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("part", [1, 3])
+def test_coefficients_that_are_none(amq, part, value):
+    """A coefficient that is NaN or infinite counts for the queries that see its token, of a few drafted ones the later, and for no other."""
+    gen = torch.Generator(device="cuda").manual_seed(27)
+    table, pages = tables(gen, 2, [600, 100], 16)
+    cache = filled(amq, gen, pages, 16, 2, 128, 4)
+    n = torch.tensor([600, 100], dtype=torch.int32, device="cuda")
+    q = torch.randn((2, 3, 4, 128), device="cuda", generator=gen)
+    want = expected(amq, q, cache, table, n, 0.1)
+    last = int(table[0, 599 // 16])                         # the newest token of the first sequence, one head of two
+    cache[part][last, 599 % 16, 1, 2] = value
+    got = amq.cache_attention(q, cache, table, n, 0.1)
+    assert torch.isnan(got[0, 2, 2:]).all()
+    got[0, 2, 2:], want[0][0, 2, 2:] = 0, 0
+    close(got, want)
+
+
 def test_a_cache_beyond_32_bit_offsets(amq):
     """Rows behind 2^31 words and 2^32 bytes of codes: a page near the end of a large cache."""
     heads, d, k, page_size = 16, 128, 4, 256
@@ -281,7 +299,7 @@ def test_append_outside_the_table(amq):
     before = [t.clone() for t in cache]
     new = [t[:1, :2].repeat(3, 1, *([1] * (t.dim() - 2))).contiguous() for t in cache]
     table = torch.tensor([[0, 1]] * 3, dtype=torch.int32, device="cuda")
-    amq.cache_append(*new, cache, table, torch.tensor([-1, 2 ** 31 - 1, 0], dtype=torch.int32, device="cuda"), 128)
+    amq.cache_append(*new, cache, table, torch.tensor([-1, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda"), 128)
     for g, w in zip(cache, before):
         assert torch.equal(g, w)
 

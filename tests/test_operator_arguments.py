@@ -112,6 +112,10 @@ def reorder(lib, src=(FAKE, FAKE), dst=(FAKE, FAKE), row=(64, 64), from_=(64, 64
 
 def test_beam_reorder(lib):
     assert reorder(lib, count=0) == OK
+    assert reorder(lib) == INVALID                                  # one state twice, in place
+    assert reorder(lib, dst=(2 * FAKE, 2 * FAKE)) == INVALID
+    assert reorder(lib, dst=(2 * FAKE, FAKE)) == INVALID            # (the second is read by the first's threads)
+    assert reorder(lib, dst=(FAKE, 2 * FAKE)) == INVALID
     assert reorder(lib, batch=0) == OK
     assert reorder(lib, row=(0, 0)) == OK
     assert reorder(lib, count=-1) == INVALID
