@@ -467,30 +467,26 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
                 for (int e = 0; e < 2; ++e) s[z][n][e] = (s[z][n][e] + __shfl_xor_sync(0xffffffffu, s[z][n][e], 16)) * factor[z];
             }
         }
-        // the values' planes: an MMA's 32 positions are 32 / pitch tokens, 8 / pitch of them this lane's
-        constexpr int PK = pitch(K);            // MMA steps of a tile
-        uint32_t bv[PK][2][2];
+        // the values' planes: K MMA steps, in whose 32 positions this lane's are the planes of its eight tokens, eight planes a step
+        uint32_t bv[K][2][2];
         {
-            uint32_t word[8][PK];               // by this lane's tokens, (n, e) = (0, 0), (0, 1), (1, 0), ..
+            uint32_t word[8 * K];               // by this lane's tokens, (n, e) = (0, 0), (0, 1), (1, 0), .., and planes
 #pragma unroll
             for (int q = 0; q < 8; ++q)
 #pragma unroll
-                for (int i = 0; i < PK; ++i)
-                    word[q][i] = i < K ? *reinterpret_cast<const uint32_t*>(words + vat[i < K ? i : 0] + ((q >> 1) * 8 + (q & 1)) * pitch(K) * 16) : 0u;
+                for (int i = 0; i < K; ++i) word[q * K + i] = *reinterpret_cast<const uint32_t*>(words + vat[i] + ((q >> 1) * 8 + (q & 1)) * pitch(K) * 16);
 #pragma unroll
-            for (int z = 0; z < PK; ++z)
+            for (int z = 0; z < K; ++z)
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
-                    uint32_t ww[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) ww[u] = word[(2 * z + side) * (4 / PK) + u / PK][u % PK];
+                    const uint32_t* const ww = word + (2 * z + side) * 4;
                     const uint32_t t0 = __byte_perm(ww[0], ww[1], half), t1 = __byte_perm(ww[2], ww[3], half);
                     bv[z][side][0] = __byte_perm(t0, t1, 0x5410);
                     bv[z][side][1] = __byte_perm(t0, t1, 0x7632);
                 }
         }
         // weights, relative to the tile's maximum, times coefficients as digits
-        uint32_t ap[MT][PK][4];
+        uint32_t ap[MT][K][4];
         float unit[MT];
         f32x2 base_2[MT], corr_2[MT];
 #pragma unroll
@@ -511,28 +507,25 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             const float corr = exp2_approx(m[z] - m_ref), tile_factor = exp2_approx(top - m_ref);
             m[z] = m_new;
             float sum = 0.0f;
-            uint32_t y[8][PK];                  // by this lane's tokens
+            uint32_t y[8 * K];                  // by this lane's tokens and planes
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const float e0 = exp2_approx(s[z][n][0] - ref), e1 = exp2_approx(s[z][n][1] - ref);
                 sum += e0 + e1;
                 const f32x2 ws = mul2(pack2(e0, e1), pack2(to_fixed, to_fixed));
 #pragma unroll
-                for (int i = 0; i < PK; ++i) {
-                    if (i >= K) { y[2 * n][i] = y[2 * n + 1][i] = 0x80808080u; continue; }
+                for (int i = 0; i < K; ++i) {
                     float f0, f1;
-                    unpack2(mul2(ws, *reinterpret_cast<const f32x2*>(&coef.v[i < K ? i : 0][8 * n + 2 * c])), f0, f1);
-                    y[2 * n][i] = (uint32_t)__float2int_rn(f0) + 0x80808080u;
-                    y[2 * n + 1][i] = (uint32_t)__float2int_rn(f1) + 0x80808080u;
+                    unpack2(mul2(ws, *reinterpret_cast<const f32x2*>(&coef.v[i][8 * n + 2 * c])), f0, f1);
+                    y[2 * n * K + i] = (uint32_t)__float2int_rn(f0) + 0x80808080u;
+                    y[(2 * n + 1) * K + i] = (uint32_t)__float2int_rn(f1) + 0x80808080u;
                 }
             }
 #pragma unroll
-            for (int q = 0; q < PK; ++q)
+            for (int q = 0; q < K; ++q)
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
-                    uint32_t yy[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) yy[u] = y[(2 * q + side) * (4 / PK) + u / PK][u % PK];
+                    const uint32_t* const yy = y + (2 * q + side) * 4;
                     ap[z][q][2 * side] = __byte_perm(__byte_perm(yy[0], yy[1], digit0), __byte_perm(yy[2], yy[3], digit0), 0x5410) ^ 0x80808080u;
                     ap[z][q][2 * side + 1] = __byte_perm(__byte_perm(yy[0], yy[1], digit1), __byte_perm(yy[2], yy[3], digit1), 0x5410) ^ 0x80808080u;
                 }
@@ -540,7 +533,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             int ones[4];
             mma_s8u8(ones, ap[z][0], 0x01010101u, 0x01010101u, start);
 #pragma unroll
-            for (int q = 1; q < PK; ++q) mma_s8u8(ones, ap[z][q], 0x01010101u, 0x01010101u);
+            for (int q = 1; q < K; ++q) mma_s8u8(ones, ap[z][q], 0x01010101u, 0x01010101u);
             unit[z] = tile_factor * from_fixed * w1;                // (w0 = 2^16 w1)
             const float base = -unit[z] * fmaf(65536.0f, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
             base_2[z] = pack2(base, base); corr_2[z] = pack2(corr, corr);
@@ -550,7 +543,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         for (int j0 = 0; j0 < 8; j0 += SIDE) {
             int acc[SIDE][2][MT][4];
 #pragma unroll
-            for (int q = 0; q < PK; ++q)
+            for (int q = 0; q < K; ++q)
 #pragma unroll
                 for (int s = 0; s < SIDE; ++s)
 #pragma unroll
@@ -682,7 +675,7 @@ struct AttentionPlan { int rows, row_tiles, row_blocks, warps, shares; long long
 // Up to 512 tokens a CTA takes a block's whole sequence, with twelve warps (a tile of tokens each or little more) where the CTAs are few: one sequence of 300
 // tokens, 8 heads: 8.7 us, with four warps 9.9.  Else the tiles are dealt out to as many CTAs as fit the GPU, or to fewer of at least 16 tiles:
 // 64 sequences of 1024 to 4096 tokens in equal numbers of shares each took 127 us, 112 so; one of 65000 tokens 94, 79 so.
-// Two row tiles to a CTA where rows fill them: 8 rows over 65000 tokens 79 us, 85 with one; 9 rows over 20 x 1500 tokens 47 us, 37 with one.
+// Two row tiles to a CTA where rows fill them: 8 rows over 65000 tokens 79 us, 85 with one; 9 rows over 20 x 1500 tokens (3 bits) 47 us, 37 with one.
 AttentionPlan attention_plan(int batch, int q_len, int q_heads, int heads, long long max_tokens)
 {
     AttentionPlan a{};
