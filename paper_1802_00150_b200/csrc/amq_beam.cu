@@ -9,9 +9,12 @@
 // A cluster of eight CTAs takes a batch entry; CTA c reads the eighth c of every beam's row, so any number of beams is balanced, and one entry
 // alone still has eight SMs.  A group of 256 threads takes a beam's eighth in pieces of up to twelve words a thread, the next piece on its way while
 // one is worked on: one word a lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's
-// sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the eighth's K-th largest logit comes from the maxima of 32 groups of
-// eight threads, and little more than K logits reach it; those are written down, sorted by counting, and go to the first CTA's shared memory, which
+// sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the eighth's K-th largest logit comes from the maxima of 32 or 64 groups
+// of threads, and little more than K logits reach it; those are written down, sorted by a warp, and go to the first CTA's shared memory, which
 // joins the eight by score.
+// Bound by instructions, 22 for a lane and logit at 21 logits a thread and row: the exponentials' four and the comparisons, and some 300 a warp and
+// row for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 29 us, 2.9 TB/s (a CTA to an entry, a pass for the sum and
+// one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 9 us, a chain of two barriers, the cluster's exchange and the join.
 #include <cooperative_groups.h>
 
 #include "amq_common.cuh"
@@ -24,7 +27,8 @@ namespace cg = cooperative_groups;
 constexpr int SLICES = 8;               // CTAs of a cluster
 constexpr int MAX_THREADS = 1024;       // of a CTA: groups of 128 or 256 threads, each with beams of its own
 constexpr int MAX_GROUPS = 8, MAX_WARPS = 8;        // groups, warps of a group
-constexpr int CAP = 128;                // candidates kept of a beam's slice; where more pass the bound (ties), the slice is searched again
+constexpr int CAP = 256;                // candidates kept of a beam's slice; where more pass the bound (ties), the slice is searched again
+constexpr int MAXIMA = 64;
 
 struct SelectParams {
     const float* logits; int ld; int vocab;
@@ -32,10 +36,10 @@ struct SelectParams {
     float* scores_out; int32_t* parents; int32_t* tokens; int32_t* finished_out;
 };
 
-// order-preserving maps to unsigned integers (NaN never passes the comparisons in front of them)
+// order-preserving maps to unsigned integers (NaN never passes the comparisons in front of them); -0 is 0
 __device__ __forceinline__ uint32_t ordered(float v)
 {
-    const uint32_t u = __float_as_uint(v);
+    const uint32_t u = __float_as_uint(v + 0.0f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
@@ -55,7 +59,6 @@ struct SelectSmem {
     WarpSum* sums;                      // [beams][SLICES][warps of a group], from every CTA
     unsigned long long* best;           // [beams][SLICES][beams], from every CTA: sorted candidates, 0 where there are fewer
     unsigned long long* list;           // [beams][CAP] as found
-    int* count;                         // [beams]
 };
 
 __host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* base)
@@ -66,10 +69,9 @@ __host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* ba
     char* sums = take(sizeof(WarpSum) * SLICES * MAX_WARPS * beams);
     char* best = take(8ull * SLICES * beams * beams);
     char* list = take(8ull * CAP * beams);
-    char* count = take(4ull * beams);
     if (s) {
         s->sums = reinterpret_cast<WarpSum*>(sums); s->best = reinterpret_cast<unsigned long long*>(best);
-        s->list = reinterpret_cast<unsigned long long*>(list); s->count = reinterpret_cast<int*>(count);
+        s->list = reinterpret_cast<unsigned long long*>(list);
     }
     return off;
 }
@@ -85,6 +87,24 @@ __device__ __forceinline__ unsigned long long ordered(double v)
 __device__ __forceinline__ double from_ordered(unsigned long long o)
 {
     return __longlong_as_double((long long)(o ^ ((o >> 63) ? 0x8000000000000000ull : 0xffffffffffffffffull)));
+}
+
+// the 32 best of `kept`, in descending order over a warp's lanes, and 32 others in any, in descending order: a bitonic sort of those, ascending, and a merge
+__device__ __forceinline__ unsigned long long best_of(unsigned long long kept, unsigned long long other)
+{
+    const int lane = threadIdx.x & 31;
+    auto exchange = [&](unsigned long long v, int stride, bool larger) {
+        const unsigned long long o = __shfl_xor_sync(0xffffffffu, v, stride);
+        return (o > v) == larger ? o : v;
+    };
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int stride = size >> 1; stride > 0; stride >>= 1) other = exchange(other, stride, ((lane & stride) != 0) == ((lane & size & 31) == 0));
+    if (other > kept) kept = other;
+#pragma unroll
+    for (int stride = 16; stride > 0; stride >>= 1) kept = exchange(kept, stride, (lane & stride) == 0);
+    return kept;
 }
 
 struct Choice { unsigned long long score; int pair; };       // score 0: none
@@ -134,7 +154,8 @@ beam_select_kernel(SelectParams p)
     __shared__ float s_score[AMQ_MAX_BEAMS];
     __shared__ int s_done[AMQ_MAX_BEAMS];
     __shared__ double s_lse[AMQ_MAX_BEAMS];
-    __shared__ uint32_t s_maxima[MAX_GROUPS][2][32];
+    __shared__ uint32_t s_maxima[MAX_GROUPS][2][MAXIMA];
+    __shared__ int s_count[AMQ_MAX_BEAMS]; __shared__ uint32_t s_bound[AMQ_MAX_BEAMS];
     __shared__ int s_found;
     __shared__ double s_chosen[AMQ_MAX_BEAMS]; __shared__ int s_chosen_pair[AMQ_MAX_BEAMS];
     cg::cluster_group cluster = cg::this_cluster();
@@ -169,7 +190,7 @@ beam_select_kernel(SelectParams p)
     for (int b = tid; b < K; b += nthreads) {
         s_score[b] = p.scores[row0 + b];
         s_done[b] = p.finished ? p.finished[row0 + b] != 0 : 0;
-        s.count[b] = 0;
+        s_count[b] = 0;
     }
     __syncthreads();
 
@@ -180,12 +201,15 @@ beam_select_kernel(SelectParams p)
     unsigned long long* const best_there = cluster.map_shared_rank(s.best, 0) + (size_t)rank * K;
 
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    if (chunks == 0)
+    if (chunks == 0) {
         for (int i = tid; i < K * WARPS; i += nthreads) sums_there[i / WARPS * SLICES * WARPS + i % WARPS] = {-INFINITY, 0.0f};
+        for (int i = tid; i < K * K; i += nthreads) best_there[(size_t)(i / K) * SLICES * K + i % K] = 0;
+    }
+
     int b = chunks ? next_open(group) : K, c = 0, buffer = 0;
     if (b < K && b != group) load(cur, b, 0);
     float m = -INFINITY, sum = 0.0f;
-    uint32_t bound = 0;                 // below every logit that counts
+    uint32_t bound = 0, highest = 0;    // below every logit that counts; this thread's largest of the row so far
     // one piece, and the next one's loads
     auto step = [&](float (&now)[PT], auto& next) {
         int nb = b, nc = c + 1;
@@ -196,12 +220,17 @@ beam_select_kernel(SelectParams p)
 #pragma unroll
         for (int i = 1; i < PT; ++i) top = fmaxf(top, now[i]);
         const uint32_t v = top > -INFINITY ? ordered(top) : 0u;
-        // (a row's second piece goes by the first one's bound: it would rarely raise it)
+        highest = max(highest, v);
+        // (a row's second piece goes by the first one's bound: another would rarely spare it much)
         if (c != 1) {
-            uint32_t of_some = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
-            of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, 2));
-            if (THREADS == 256) of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, 4));
-            if ((lane & (THREADS / 32 - 1)) == 0) s_maxima[group][buffer][at_group / (THREADS / 32)] = of_some;
+            uint32_t of_some = max(highest, __shfl_xor_sync(0xffffffffu, highest, 1));
+            if (THREADS == 256) of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, 2));
+            if (K <= 8) {               // 32 maxima, else 64
+                of_some = max(of_some, __shfl_xor_sync(0xffffffffu, of_some, THREADS / 64));
+                if ((lane & (THREADS / 32 - 1)) == 0) s_maxima[group][buffer][at_group / (THREADS / 32)] = of_some;
+            } else if ((lane & (THREADS / 64 - 1)) == 0) {
+                s_maxima[group][buffer][at_group / (THREADS / 64)] = of_some;
+            }
         }
         const float m_new = fmaxf(m, top * LOG2E), ref = m_new == -INFINITY ? 0.0f : m_new;
         sum *= exp2_ftz(m - ref);
@@ -210,32 +239,46 @@ beam_select_kernel(SelectParams p)
         m = m_new;
         if (c != 1) {
             asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
-            // The bound: up to four beams the smallest of four maxima (of a quarter of the threads; 8 logits reach it on average, 50 once in a
-            // million), else the K-th of the 32, one by one (9 for eight beams).  The two buffers in turn: who writes one again has passed the barrier
-            // behind everybody's reading of it.
+            // The bound, one that K threads' largest logits reach.  Up to four beams the smallest of four maxima (of a quarter of the threads; 8 logits
+            // reach it on average, 50 once in a million), up to eight the smallest of four second largest, of eight maxima each (14; one by one, the
+            // K-th largest of 32 took 32.5 us where this takes 28.9), else a value that K to 5 K / 4 of 64 maxima reach, by bisection.  The two
+            // buffers in turn: who writes one again has passed the barrier behind everybody's reading of it.
             uint32_t left = s_maxima[group][buffer][lane];
-            buffer ^= 1;
             if (K <= 4) {
                 left = max(left, __shfl_xor_sync(0xffffffffu, left, 4));
                 left = max(left, __shfl_xor_sync(0xffffffffu, left, 8));
                 left = max(left, __shfl_xor_sync(0xffffffffu, left, 16));
                 bound = max(bound, __reduce_min_sync(0xffffffffu, left));
-            } else if (redux_max(left) > bound) {
-                uint32_t kth = 0;
-                for (int r = 0; r < K; ++r) {
-                    kth = redux_max(left);
-                    const uint32_t has = __ballot_sync(0xffffffffu, left == kth);
-                    if (lane == __ffs(has) - 1) left = 0u;
+            } else if (K <= 8) {
+                uint32_t second = 0;
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) {
+                    const uint32_t l2 = __shfl_xor_sync(0xffffffffu, left, off), s2 = off == 4 ? 0u : __shfl_xor_sync(0xffffffffu, second, off);
+                    second = max(min(left, l2), off == 4 ? 0u : max(second, s2));
+                    left = max(left, l2);
                 }
-                bound = max(bound, kth);
+                bound = max(bound, __reduce_min_sync(0xffffffffu, second));
+            } else {
+                const uint32_t right = s_maxima[group][buffer][32 + lane];
+                // K reach `from` (or it is the bound already), fewer `to` + 1
+                uint32_t from = max(bound, __reduce_min_sync(0xffffffffu, min(left, right))), to = redux_max(max(left, right));
+                while (from < to) {
+                    const uint32_t mid = from + (to - from + 1) / 2;
+                    const int n = __popc(__ballot_sync(0xffffffffu, left >= mid)) + __popc(__ballot_sync(0xffffffffu, right >= mid));
+                    if (n >= K) from = mid;
+                    else to = mid - 1;
+                    if (n >= K && n <= K + K / 4) break;
+                }
+                bound = from;
             }
+            buffer ^= 1;
         }
         if (v && v >= bound) {
             const float least = bound ? from_ordered(bound) : -3.402823466e38f;      // (no bound yet: everything but -inf)
 #pragma unroll
             for (int i = 0; i < PT; ++i) {
                 if (now[i] >= least) {
-                    const int to = atomicAdd(&s.count[b], 1);
+                    const int to = atomicAdd(&s_count[b], 1);
                     if (to < CAP) s.list[b * CAP + to] = candidate(now[i], lo + c * CHUNK + at_group + i * THREADS);
                 }
             }
@@ -248,7 +291,8 @@ beam_select_kernel(SelectParams p)
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
             if (lane == 0) sums_there[b * SLICES * WARPS + warp] = {M, t};
-            m = -INFINITY; sum = 0.0f; bound = 0;
+            if (at_group == 0) s_bound[b] = bound;
+            m = -INFINITY; sum = 0.0f; bound = 0; highest = 0;
         }
         b = nb; c = nc;
     };
@@ -258,47 +302,45 @@ beam_select_kernel(SelectParams p)
     }
     __syncthreads();
 
-    // the K best of each beam's slice, in order: a candidate's place is the number of candidates before it
+    // the K best of each beam's slice, in order, a warp a beam
     for (int q = tid >> 5; q < K; q += nthreads >> 5) {
-        const int n = s.count[q];
+        const int n = s_count[q];
+        const unsigned long long* list = s.list + q * CAP;
         unsigned long long* best = best_there + (size_t)q * SLICES * K;
-        if (n <= 32) {                  // (as a rule)
-            const unsigned long long mine = lane < n ? s.list[q * CAP + lane] : 0ull;
+        if (n <= 32) {                  // (as a rule: a candidate's place is the number of candidates before it)
+            const unsigned long long mine = lane < n ? list[lane] : 0ull;
             int before = 0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) before += __shfl_sync(0xffffffffu, mine, j) > mine;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) before += __shfl_sync(0xffffffffu, mine, j) > mine;
             if (before < K && mine) best[before] = mine;
             if (lane >= n && lane < K) best[lane] = 0;
         } else if (n <= CAP) {
-            for (int r = (n < K ? n : K) + lane; r < K; r += 32) best[r] = 0;
-            for (int i = lane; i < n; i += 32) {
-                const unsigned long long mine = s.list[q * CAP + i];
-                int place = 0;
-#pragma unroll 4
-                for (int j = 0; j < n; ++j) place += s.list[q * CAP + j] > mine;
-                if (place < K) best[place] = mine;
-            }
-        } else {                        // more ties than the list holds: one search of the slice for every place
+            unsigned long long kept = 0;
+            for (int i = lane; i - lane < n; i += 32) kept = best_of(kept, i < n ? list[i] : 0ull);
+            if (lane < K) best[lane] = kept;
+        } else {                        // more ties than the list holds: the slice once more, past the best so far, a place of which each lane keeps
             const float* z = p.logits + (row0 + q) * p.ld;
-            unsigned long long last = ~0ull;
-            for (int r = 0; r < K; ++r) {
-                unsigned long long top = 0;
-                for (int t = lo + lane; t < hi; t += 32) {
-                    const float x = __ldcg(z + t);
-                    if (!(x > -INFINITY)) continue;
-                    const unsigned long long k = candidate(x, t);
-                    if (k < last && k > top) top = k;
-                }
+            const uint32_t least = s_bound[q];
+            unsigned long long kept = 0;
+            for (int t0 = lo; t0 < hi; t0 += 128) {
+                float x[4];
 #pragma unroll
-                for (int off = 16; off > 0; off >>= 1) {
-                    const unsigned long long o = __shfl_xor_sync(0xffffffffu, top, off);
-                    if (o > top) top = o;
+                for (int i = 0; i < 4; ++i) x[i] = t0 + 32 * i + lane < hi ? __ldcg(z + t0 + 32 * i + lane) : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned long long k = x[i] > -INFINITY && ordered(x[i]) >= least ? candidate(x[i], t0 + 32 * i + lane) : 0ull;
+                    uint32_t above = __ballot_sync(0xffffffffu, k > __shfl_sync(0xffffffffu, kept, K - 1));
+                    for (; above; above &= above - 1) {
+                        const unsigned long long one = __shfl_sync(0xffffffffu, k, __ffs(above) - 1), up = __shfl_up_sync(0xffffffffu, kept, 1);
+                        const int place = __popc(__ballot_sync(0xffffffffu, kept > one));
+                        kept = lane < place ? kept : lane == place ? one : up;
+                    }
                 }
-                if (lane == 0) best[r] = top;
-                last = top;
             }
+            if (lane < K) best[lane] = kept;
         }
     }
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     if (rank != 0) return;              // (nobody reads another CTA's shared memory, and the first one stays)
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -391,9 +433,10 @@ amq_status launch_select_groups(const SelectParams& p, int batch, int groups, cu
 
 amq_status launch_select(const SelectParams& p, int batch, cudaStream_t st)
 {
-    // beams at a time: as many as leave the CTAs of all entries on the GPU at once
+    // Beams at a time: as many as leave the CTAs of all entries on the GPU at once.  Beyond 16 the lists' memory leaves an SM few CTAs, and four beams at a time
+    // make up for that (64 entries, 32 beams, 9999 tokens: 134 us, 257 with one).
     if (batch * SLICES <= 148) return p.beams > 4 ? launch_select_groups<128>(p, batch, 8, st) : launch_select_groups<256>(p, batch, 4, st);
-    return launch_select_groups<256>(p, batch, batch * SLICES <= 296 ? 2 : 1, st);
+    return launch_select_groups<256>(p, batch, p.beams > 16 ? 4 : batch * SLICES <= 296 ? 2 : 1, st);
 }
 
 // ---- reordering ------------------------------------------------------------------------------------------------------

@@ -90,6 +90,27 @@ def test_equal_logits_go_to_the_first(amq, beams, vocab):
     assert torch.equal(got[2], torch.where(row % 2 == 0, vocab - 1, 0).int())
 
 
+@pytest.mark.parametrize("batch,beams,vocab", [(1, 8, 128000), (16, 20, 42000), (38, 32, 9999), (2, 12, 300000), (40, 6, 1000), (40, 9, 1000), (3, 4, 100001),
+                                               (1, 32, 260)])
+def test_order_within_a_row(amq, batch, beams, vocab):
+    """Rows of any order: the largest last (every piece passes what the one before it left as a bound), first, in a few places of many, all but a few -inf."""
+    gen = torch.Generator(device="cuda").manual_seed(batch * beams + vocab)
+    logits = torch.randn((batch * beams, vocab), device="cuda", generator=gen) * 2.5
+    scores = -20 * torch.rand((batch, beams), device="cuda", generator=gen)
+    up = torch.sort(logits, dim=1).values
+    for z in (up, up.flip(1).contiguous(), torch.cat((up[:, vocab // 3:], up[:, :vocab // 3]), 1).contiguous(), torch.where(logits > 0, logits.round(), 0.0),
+              torch.where(logits > 9, logits, -torch.inf), torch.where(logits > 9, 0.0, logits.clamp(max=-0.0))):
+        same(amq.beam_select(z, scores), expected(z, scores, None, -1))
+
+
+def test_zeros_of_either_sign_are_alike(amq):
+    logits = torch.full((4, 5000), -3.0, device="cuda")
+    logits[:, 7::11] = -0.0
+    logits[:, 4::23] = 0.0
+    scores = torch.tensor([[-1.0, -2.0, -3.0, -4.0]], device="cuda")
+    same(amq.beam_select(logits, scores), expected(logits, scores, None, -1))
+
+
 def test_masked_tokens_and_dead_beams(amq):
     gen = torch.Generator(device="cuda").manual_seed(6)
     batch, beams, vocab, eos = 6, 4, 700, 9
