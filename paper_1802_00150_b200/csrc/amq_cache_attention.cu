@@ -622,66 +622,89 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
   }
 }
 
-// Joins the pieces of the blocks that shares' edges cut, and writes zeros for sequences without tokens (no share has them): one CTA per row.
+// Joins the pieces of the blocks that shares' edges cut: one CTA per row, of every sequence or, where there are fewer, of every edge (that of a sequence's first
+// does the work; the kernel took 32 us by sequences for 256 of them, a quarter of the whole call).  And writes zeros for sequences without tokens, which no
+// share has.
+__host__ __device__ inline bool joins_by_sequences(int batch, int shares) { return batch < shares || shares == 1; }
+
 __global__ void __launch_bounds__(AMQ_MAX_HEAD_DIM)
 cache_attention_join_kernel(const __grid_constant__ AttentionParams p, int block_rows)
 {
     grid_dependency_wait();
-    const int units = p.c.heads * p.row_blocks, b = blockIdx.x / units, block = blockIdx.x % units, rb = block % p.row_blocks, kv = block / p.row_blocks;
+    const int units = p.c.heads * p.row_blocks, at = blockIdx.x / units, block = blockIdx.x % units, rb = block % p.row_blocks, kv = block / p.row_blocks;
     const int q = blockIdx.y, rho = rb * block_rows + q;
     if (rho >= p.rows) return;
-    const int tiles = tiles_of(p.c, b), lane = threadIdx.x & 31;
-    // this block's place in the line, and the shares that have its first and last tile
-    long long front = 0;
-    for (int b0 = 0; b0 < b; b0 += 32) {
-        const int n = b0 + lane < b ? tiles_of(p.c, b0 + lane) : 0;
-        front += (long long)__reduce_add_sync(0xffffffffu, (uint32_t)n & 0xffffu) + ((long long)__reduce_add_sync(0xffffffffu, (uint32_t)n >> 16) << 16);
-    }
-    const long long total = total_tiles(p), x = front;
-    const int shares = shares_of(p, total);
-    auto share_of = [&](long long at) {
-        long long s = at * shares / total;
-        while (total * (s + 1) / shares <= at) ++s;
-        while (total * s / shares > at) --s;
-        return (int)s;
+    const int lane = threadIdx.x & 31;
+    auto write = [&](int b, float v) {
+        const size_t orow = ((size_t)b * p.q_len + rho / p.group) * p.q_heads + kv * p.group + rho % p.group;
+        if ((int)threadIdx.x < p.c.d) p.out[orow * p.c.d + threadIdx.x] = v;
     };
-    int first = 0, last = 0;
-    if (tiles) { first = share_of(x); last = share_of(x + tiles - 1); }
-    if (tiles && first == last) return;                 // (written where it was computed)
+    const bool by_sequences = joins_by_sequences(p.batch, p.shares);
+    for (int b0 = at, step = by_sequences ? p.batch : p.shares - 1; b0 < p.batch; b0 += 32 * step) {
+        const int e = b0 + lane * step;
+        for (uint32_t empty = __ballot_sync(0xffffffffu, e < p.batch && tiles_of(p.c, e) == 0); empty; empty &= empty - 1) write(b0 + (__ffs(empty) - 1) * step, 0.0f);
+    }
+    const long long total = total_tiles(p);
+    const int shares = shares_of(p, total);
+    auto edge = [&](int s) { return total * s / shares; };
+    long long x = 0;                    // the sequence's place in the line
+    int b = at, first;                  // the share that has its first tile
+    if (by_sequences) {
+        for (int b0 = 0; b0 < b; b0 += 32) {
+            const int n = b0 + lane < b ? tiles_of(p.c, b0 + lane) : 0;
+            x += (long long)__reduce_add_sync(0xffffffffu, (uint32_t)n & 0xffffu) + ((long long)__reduce_add_sync(0xffffffffu, (uint32_t)n >> 16) << 16);
+        }
+        if (tiles_of(p.c, b) == 0) return;
+        first = (int)(x * shares / total);
+        while (edge(first + 1) <= x) ++first;
+        while (edge(first) > x) --first;
+    } else {
+        first = at;
+        if (first + 1 >= shares) return;
+        b = sequence_at(p, edge(first + 1), &x);
+        if (edge(first + 1) == x || edge(first) > x) return;        // (nothing is cut here; cut by an edge before this one)
+    }
+    const long long end = x + tiles_of(p.c, b);
+    int last = first;
+    if (edge(first + 1) < end) {
+        last = (int)((end - 1) * shares / total);
+        while (edge(last + 1) < end) ++last;
+        while (edge(last) >= end) --last;
+    }
+    if (first == last) return;          // (written where it was computed)
     float M = -INFINITY, sum = 0.0f, v = 0.0f;
     auto part = [&](int s) { return (((size_t)s * units + block) * 2 + (s == first ? 1 : 0)) * block_rows + q; };
-    if (tiles) {
-        for (int s0 = first; s0 <= last; s0 += 32) M = fmaxf(M, s0 + lane <= last ? __ldcg(p.part_ml + part(s0 + lane)).x : -INFINITY);
+    for (int s0 = first; s0 <= last; s0 += 32) M = fmaxf(M, s0 + lane <= last ? __ldcg(p.part_ml + part(s0 + lane)).x : -INFINITY);
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-        const float m_ref = M == -INFINITY ? 0.0f : M;
-        for (int s0 = first; s0 <= last; s0 += 32) {
-            const float2 ml = s0 + lane <= last ? __ldcg(p.part_ml + part(s0 + lane)) : make_float2(-INFINITY, 0.0f);
-            const float f = exp2_approx(ml.x - m_ref);
-            sum += ml.y * f;
-            const int n = min(32, last - s0 + 1);
+    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    const float m_ref = M == -INFINITY ? 0.0f : M;
+    for (int s0 = first; s0 <= last; s0 += 32) {
+        const float2 ml = s0 + lane <= last ? __ldcg(p.part_ml + part(s0 + lane)) : make_float2(-INFINITY, 0.0f);
+        const float f = exp2_approx(ml.x - m_ref);
+        sum += ml.y * f;
+        const int n = min(32, last - s0 + 1);
 #pragma unroll 8
-            for (int s = 0; s < n; ++s) v += __ldcg(p.part + part(s0 + s) * AMQ_MAX_HEAD_DIM + threadIdx.x) * __shfl_sync(0xffffffffu, f, s);
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        for (int s = 0; s < n; ++s) v += __ldcg(p.part + part(s0 + s) * AMQ_MAX_HEAD_DIM + threadIdx.x) * __shfl_sync(0xffffffffu, f, s);
     }
-    const size_t orow = ((size_t)b * p.q_len + rho / p.group) * p.q_heads + kv * p.group + rho % p.group;
-    if ((int)threadIdx.x < p.c.d) p.out[orow * p.c.d + threadIdx.x] = sum == 0.0f ? 0.0f : v / sum;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    write(b, sum == 0.0f ? 0.0f : v / sum);
 }
 
 struct AttentionPlan { int rows, row_tiles, row_blocks, warps, shares; long long blocks; size_t part_bytes, bytes; };
 
-// Up to 512 tokens a CTA takes a block's whole sequence, with twelve warps (a tile of tokens each or little more) where the CTAs are few: one sequence of 300
-// tokens, 8 heads: 8.7 us, with four warps 9.9.  Else the tiles are dealt out to as many CTAs as fit the GPU, or to fewer of at least 16 tiles:
-// 64 sequences of 1024 to 4096 tokens in equal numbers of shares each took 127 us, 112 so; one of 65000 tokens 94, 79 so.
+// Up to 1024 tokens a CTA takes a block's whole sequence, with twelve warps (a tile of tokens each or little more) where the CTAs are few: one sequence of
+// 300 tokens, 8 heads: 9.2 us, with four warps 9.9.  Else the tiles are dealt out to as many CTAs as fit the GPU, or to fewer of at least 16 tiles.
+// Sequences of 1024 tokens, 8 heads, 4 query heads each, whole and in shares: one 16.5 and 17.2 us, 16 17.4 and 22.5, 64 48 and 57, 256 151 and 180;
+// of 2048: 8 28.7 and 23, 32 of 512 to 2048 48 and 42.  64 sequences of 1024 to 4096 tokens in equal numbers of shares each took 127 us, dealt out
+// 112; one of 65000 tokens 94 and 79.
 // Two row tiles to a CTA where rows fill them: 8 rows over 65000 tokens 79 us, 85 with one; 9 rows over 20 x 1500 tokens (3 bits) 47 us, 37 with one.
 AttentionPlan attention_plan(int batch, int q_len, int q_heads, int heads, long long max_tokens)
 {
     AttentionPlan a{};
     a.rows = q_len * (q_heads / heads);
     const int row_tiles = (a.rows + ROWS - 1) / ROWS;
-    const bool whole = max_tokens <= 512;
+    const bool whole = max_tokens <= 1024;
     a.row_tiles = !whole && row_tiles % 2 == 0 ? 2 : 1;
     const int block = a.row_tiles * ROWS;
     a.row_blocks = (a.rows + block - 1) / block;
@@ -764,7 +787,8 @@ amq_status amq_cache_attention(const float* q, long long q_batch, long long q_to
         default: s = amq::launch_attention_as<4>(p, plan, (unsigned)grid, st); break;
     }
     if (s != AMQ_OK || plan.shares == 0) return s;
-    AMQ_CUDA_TRY(amq::launch_kernel(amq::cache_attention_join_kernel, dim3((unsigned)plan.blocks, (unsigned)(plan.row_tiles * amq::ROWS)), dim3(AMQ_MAX_HEAD_DIM), 0, st, true, p,
+    const long long join_blocks = plan.blocks / batch * (amq::joins_by_sequences(batch, plan.shares) ? batch : plan.shares - 1);
+    AMQ_CUDA_TRY(amq::launch_kernel(amq::cache_attention_join_kernel, dim3((unsigned)join_blocks, (unsigned)(plan.row_tiles * amq::ROWS)), dim3(AMQ_MAX_HEAD_DIM), 0, st, true, p,
                                     plan.row_tiles * amq::ROWS));
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;

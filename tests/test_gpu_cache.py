@@ -241,6 +241,26 @@ def test_a_table_with_room_for_more(amq, lengths, k, group):
     close(amq.cache_attention(q, cache, table, n, 0.1, ws), want)
 
 
+@pytest.mark.parametrize("batch,heads,group,q_len,most,none", [(150, 8, 4, 2, 200, 0.4), (90, 2, 3, 1, 1200, 0.1), (700, 1, 1, 1, 40, 0.0), (140, 8, 1, 1, 700, 0.9),
+                                                               (5, 32, 4, 48, 300, 0.4), (75, 8, 4, 1, 2500, 0.2)])
+def test_more_sequences_than_shares(amq, batch, heads, group, q_len, most, none):
+    """Sequences without tokens among many, one to several in a share, and head counts that leave the line of tokens whole."""
+    gen = torch.Generator(device="cuda").manual_seed(batch)
+    n = torch.randint(1, most, (batch,), device="cuda", generator=gen, dtype=torch.int32)
+    n[torch.rand((batch,), device="cuda", generator=gen) < none] = 0
+    small, pages = tables(gen, batch, n.tolist(), 16)
+    cache = filled(amq, gen, pages, 16, heads, 64, 2)
+    table = torch.full((batch, 160), -1, dtype=torch.int32, device="cuda")
+    table[:, :small.shape[1]] = small
+    q = torch.randn((batch, q_len, heads * group, 64), device="cuda", generator=gen)
+    want = expected(amq, q, cache, table, n, 0.1)
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    bytes_ = amq.cache_attention_workspace_bytes(batch, q_len, heads * group, heads, 64, 160 * 16)
+    assert bytes_
+    ws = torch.full((bytes_,), 255, dtype=torch.uint8, device="cuda")           # (NaN, should it be read)
+    close(amq.cache_attention(q, cache, table, n, 0.1, ws, out), want)
+
+
 def test_attention_in_a_graph_and_on_another_stream(amq):
     gen = torch.Generator(device="cuda").manual_seed(25)
     lengths = [3000, 17]
