@@ -444,18 +444,18 @@ amq_status launch_select(const SelectParams& p, int batch, cudaStream_t st)
 struct ReorderParams {
     const char* src[AMQ_MAX_STATES]; char* dst[AMQ_MAX_STATES];
     long long src_stride[AMQ_MAX_STATES], dst_stride[AMQ_MAX_STATES];
-    int columns[AMQ_MAX_STATES];        // words of type V in a row
+    int columns[AMQ_MAX_STATES];        // words in a row
+    uint32_t wide;                      // states whose rows are words of 16 bytes (a bit each), the others' are of 4
     const int32_t* parents;
     int batch, beams;
 };
 
 // A thread owns one column of a batch entry across all its beams: it reads the parents' values first and writes after, so the states may be
-// reordered in place without a second copy.  K: registers for the beams.
+// reordered in place without a second copy.  K: registers for the beams.  Bound by memory: four states of 256 x 8 rows of 2048 floats, 67 MB each way, 17 us, 8.0 TB/s
+// (what is written is partly still in L2 when the kernel ends); rows of 2047 floats, in words of 4 bytes, 26 to 28 us.
 template <typename V, int K>
-__global__ void __launch_bounds__(256)
-beam_reorder_kernel(const __grid_constant__ ReorderParams p)
+__device__ __forceinline__ void reorder_columns(const ReorderParams& p)
 {
-    grid_dependency_wait();
     const int st = blockIdx.y, columns = p.columns[st];
     const long long all = (long long)p.batch * columns;
     for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < all; at += (long long)gridDim.x * 256) {
@@ -465,6 +465,7 @@ beam_reorder_kernel(const __grid_constant__ ReorderParams p)
         char* dst = p.dst[st] + row0 * p.dst_stride[st] + (long long)column * sizeof(V);
         V v[K];
         int parent[K];
+        uint32_t moves = 0;             // beams that are written: all, in place those of another parent
 #pragma unroll
         for (int b = 0; b < K; ++b)
             if (b < p.beams) {
@@ -473,18 +474,31 @@ beam_reorder_kernel(const __grid_constant__ ReorderParams p)
             }
 #pragma unroll
         for (int b = 0; b < K; ++b)
-            if (b < p.beams) v[b] = *reinterpret_cast<const V*>(src + parent[b] * p.src_stride[st]);
+            if (b < p.beams) {
+                v[b] = *reinterpret_cast<const V*>(src + parent[b] * p.src_stride[st]);
+                if (parent[b] != b || src != dst) moves |= 1u << b;
+            }
 #pragma unroll
         for (int b = 0; b < K; ++b)
-            if (b < p.beams && (parent[b] != b || src != dst)) *reinterpret_cast<V*>(dst + b * p.dst_stride[st]) = v[b];
+            if (moves >> b & 1) *reinterpret_cast<V*>(dst + b * p.dst_stride[st]) = v[b];
     }
 }
 
-template <typename V>
-amq_status launch_reorder(const ReorderParams& p, int count, cudaStream_t st)
+// WIDE, NARROW: whether there are states of either kind (words of 4 bytes alone need fewer registers: 26 us above, 32 with both)
+template <int K, bool WIDE, bool NARROW>
+__global__ void __launch_bounds__(256)
+beam_reorder_kernel(const __grid_constant__ ReorderParams p)
 {
-    auto kernel = p.beams <= 4 ? beam_reorder_kernel<V, 4> : p.beams <= 8 ? beam_reorder_kernel<V, 8>
-                : p.beams <= 16 ? beam_reorder_kernel<V, 16> : beam_reorder_kernel<V, 32>;
+    grid_dependency_wait();
+    if (WIDE && (!NARROW || (p.wide >> blockIdx.y & 1))) reorder_columns<uint4, K>(p);
+    else reorder_columns<uint32_t, K>(p);
+}
+
+template <bool WIDE, bool NARROW>
+amq_status launch_reorder_as(const ReorderParams& p, int count, cudaStream_t st)
+{
+    auto kernel = p.beams <= 4 ? beam_reorder_kernel<4, WIDE, NARROW> : p.beams <= 8 ? beam_reorder_kernel<8, WIDE, NARROW>
+                : p.beams <= 16 ? beam_reorder_kernel<16, WIDE, NARROW> : beam_reorder_kernel<32, WIDE, NARROW>;
     long long most = 0;
     for (int i = 0; i < count; ++i) if (p.columns[i] > most) most = p.columns[i];
     long long blocks = (most * p.batch + 255) / 256;
@@ -492,6 +506,12 @@ amq_status launch_reorder(const ReorderParams& p, int count, cudaStream_t st)
     AMQ_CUDA_TRY(launch_kernel(kernel, dim3((unsigned)blocks, (unsigned)count), dim3(256), 0, st, true, p));
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;
+}
+
+amq_status launch_reorder(const ReorderParams& p, int count, cudaStream_t st)
+{
+    if (p.wide == 0) return launch_reorder_as<false, true>(p, count, st);
+    return p.wide == (1u << count) - 1u ? launch_reorder_as<true, false>(p, count, st) : launch_reorder_as<true, true>(p, count, st);
 }
 
 }  // namespace
@@ -519,14 +539,13 @@ amq_status amq_beam_reorder(const void* const* src, void* const* dst, const size
     if (!src || !dst || !row_bytes || !src_stride || !dst_stride || !parents) return AMQ_ERR_INVALID_ARG;
     amq::ReorderParams p{};
     p.parents = parents; p.batch = batch; p.beams = beams;
-    bool wide = true;                   // every row of every state in 16-byte words
     for (int i = 0; i < count; ++i) {
         if (src_stride[i] < row_bytes[i] || dst_stride[i] < row_bytes[i] || (src[i] == dst[i] && src_stride[i] != dst_stride[i])) return AMQ_ERR_INVALID_ARG;
         if (row_bytes[i] && (!src[i] || !dst[i])) return AMQ_ERR_INVALID_ARG;
         if (row_bytes[i] / 4 > 0x7fffffffu) return AMQ_ERR_UNSUPPORTED;
         const uintptr_t bits = reinterpret_cast<uintptr_t>(src[i]) | reinterpret_cast<uintptr_t>(dst[i]) | row_bytes[i] | src_stride[i] | dst_stride[i];
         if (bits & 3) return AMQ_ERR_ALIGNMENT;
-        if (bits & 15) wide = false;
+        if ((bits & 15) == 0) p.wide |= 1u << i;
         p.src[i] = static_cast<const char*>(src[i]); p.dst[i] = static_cast<char*>(dst[i]);
         p.src_stride[i] = (long long)src_stride[i]; p.dst_stride[i] = (long long)dst_stride[i];
     }
@@ -536,11 +555,11 @@ amq_status amq_beam_reorder(const void* const* src, void* const* dst, const size
             if (i != j && row_bytes[i] && row_bytes[j] && (dst[i] == dst[j] || dst[i] == src[j])) return AMQ_ERR_INVALID_ARG;
     long long most = 0;
     for (int i = 0; i < count; ++i) {
-        p.columns[i] = (int)(row_bytes[i] / (wide ? 16 : 4));
+        p.columns[i] = (int)(row_bytes[i] / (p.wide >> i & 1 ? 16 : 4));
         if (p.columns[i] > most) most = p.columns[i];
     }
     if (most == 0) return AMQ_OK;
-    return wide ? amq::launch_reorder<uint4>(p, count, (cudaStream_t)stream) : amq::launch_reorder<uint32_t>(p, count, (cudaStream_t)stream);
+    return amq::launch_reorder(p, count, (cudaStream_t)stream);
 }
 
 }  // extern "C"
