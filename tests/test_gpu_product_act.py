@@ -106,6 +106,19 @@ def test_values_that_saturate(amq, batch):
         assert (y[:, 0] == hi).all() and (y[:, 1] == lo).all(), name
 
 
+@pytest.mark.parametrize("m,n,batch", [(4, 64, 1), (4, 64, 3), (2048, 256, 200), (1024, 1024, 64)])
+def test_infinite_sums(amq, m, n, batch):
+    """The activations' limits, and NaN as NaN."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    W, x = packed(amq, gen, m, n, 2), packed(amq, gen, batch, n, 2)
+    inf = float("inf")
+    bias = torch.tensor([inf, -inf, float("nan"), 3e38], device="cuda").repeat(m // 4)
+    for name, hi, lo in (("NONE", inf, -inf), ("RELU", inf, 0.0), ("GELU", inf, 0.0), ("SILU", inf, 0.0), ("TANH", 1.0, -1.0), ("SIGMOID", 1.0, 0.0)):
+        y = amq.binary_gemm_act(*W, *x, n, bias=bias, activation=getattr(amq, "ACT_" + name))
+        assert (y[:, 0::4] == hi).all() and (y[:, 1::4] == lo).all() and torch.isnan(y[:, 2::4]).all(), name
+        assert (y[:, 3::4] == (min(hi, bias[3]))).all(), name
+
+
 def test_refused_tensors(amq):
     gen = torch.Generator(device="cuda").manual_seed(3)
     W, x = packed(amq, gen, 8, 64, 2), packed(amq, gen, 2, 64, 2)
