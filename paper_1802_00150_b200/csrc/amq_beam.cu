@@ -6,14 +6,14 @@
 // exponentials together, and only beams x 8 x beams candidates are compared by score, in double: candidates of two beams may lie closer
 // than fp32 rounding of a score of -20 (2e-6), those of one beam never change places.
 //
-// A cluster of eight CTAs takes a batch entry; CTA c reads the eighth c of every beam's row, so any number of beams is balanced, and one entry
-// alone still has eight SMs.  A group of 256 threads takes a beam's eighth in pieces of up to twelve words a thread, the next piece on its way while
-// one is worked on: one word a lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's
-// sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the eighth's K-th largest logit comes from the maxima of 32 or 64 groups
+// A cluster of eight or four CTAs takes a batch entry; CTA c reads the share c of every beam's row, so any number of beams is balanced, and one entry
+// alone still has eight SMs.  A group of 128 or 256 threads takes a beam's share in pieces of up to 24 words a thread, with up to twelve the next piece on its
+// way while one is worked on: one word a lane and load, coalesced at any alignment, so that rows of an odd vocabulary cost nothing and the order of a row's
+// sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the share's K-th largest logit comes from the maxima of 32 or 64 groups
 // of threads, and little more than K logits reach it; those are written down, sorted by a warp, and go to the first CTA's shared memory, which
-// joins the eight by score.
+// joins them by score.
 // Bound by instructions, 22 for a lane and logit at 21 logits a thread and row: the exponentials' four and the comparisons, and some 300 a warp and
-// row for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 29 us, 2.9 TB/s (a CTA to an entry, a pass for the sum and
+// row for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.5 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
 // one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 9 us, a chain of two barriers, the cluster's exchange and the join.
 #include <cooperative_groups.h>
 
@@ -24,7 +24,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int SLICES = 8;               // CTAs of a cluster
 constexpr int MAX_THREADS = 1024;       // of a CTA: groups of 128 or 256 threads, each with beams of its own
 constexpr int MAX_GROUPS = 8, MAX_WARPS = 8;        // groups, warps of a group
 constexpr int CAP = 256;                // candidates kept of a beam's slice; where more pass the bound (ties), the slice is searched again
@@ -56,18 +55,18 @@ struct WarpSum { float m, s; };
 
 // shared memory of a CTA.  What the others send lies in the first CTA's.
 struct SelectSmem {
-    WarpSum* sums;                      // [beams][SLICES][warps of a group], from every CTA
-    unsigned long long* best;           // [beams][SLICES][beams], from every CTA: sorted candidates, 0 where there are fewer
+    WarpSum* sums;                      // [beams][slices][warps of a group], from every CTA
+    unsigned long long* best;           // [beams][slices][beams], from every CTA: sorted candidates, 0 where there are fewer
     unsigned long long* list;           // [beams][CAP] as found
 };
 
-__host__ __device__ inline size_t select_smem(int beams, SelectSmem* s, void* base)
+__host__ __device__ inline size_t select_smem(int slices, int beams, SelectSmem* s, void* base)
 {
     char* p = static_cast<char*>(base);
     size_t off = 0;
     auto take = [&](size_t bytes) { char* at = p + off; off += (bytes + 15) / 16 * 16; return at; };
-    char* sums = take(sizeof(WarpSum) * SLICES * MAX_WARPS * beams);
-    char* best = take(8ull * SLICES * beams * beams);
+    char* sums = take(sizeof(WarpSum) * slices * MAX_WARPS * beams);
+    char* best = take(8ull * slices * beams * beams);
     char* list = take(8ull * CAP * beams);
     if (s) {
         s->sums = reinterpret_cast<WarpSum*>(sums); s->best = reinterpret_cast<unsigned long long*>(best);
@@ -112,9 +111,9 @@ struct Choice { unsigned long long score; int pair; };       // score 0: none
 // One warp joins the sorted lists (one for each beam and slice): LISTS of them a lane, and beam after beam of the result the best of their heads,
 // by score, then pair.  `score_of(list, place)`.  Returns how many there were; lane 0 has written them down.
 template <int LISTS, typename F>
-__device__ __forceinline__ int join_lists(int K, F&& score_of, double* chosen, int* chosen_pair)
+__device__ __forceinline__ int join_lists(int K, int lists, F&& score_of, double* chosen, int* chosen_pair)
 {
-    const int lane = threadIdx.x & 31, lists = K * SLICES;
+    const int lane = threadIdx.x & 31;
     Choice head[LISTS];
     int place[LISTS];
 #pragma unroll
@@ -143,8 +142,8 @@ __device__ __forceinline__ int join_lists(int K, F&& score_of, double* chosen, i
     return K;
 }
 
-// THREADS: of a group; PT: words of a thread and piece
-template <int THREADS, int PT>
+// SLICES: CTAs of a cluster; THREADS: of a group; PT: words of a thread and piece
+template <int SLICES, int THREADS, int PT>
 __global__ void __cluster_dims__(SLICES, 1, 1) __launch_bounds__(MAX_THREADS, 1)
 beam_select_kernel(SelectParams p)
 {
@@ -162,7 +161,7 @@ beam_select_kernel(SelectParams p)
     const int K = p.beams, tid = threadIdx.x, nthreads = blockDim.x, lane = tid & 31;
     const int groups = nthreads / THREADS, group = tid / THREADS, at_group = tid % THREADS, warp = at_group >> 5;
     SelectSmem s;
-    select_smem(K, &s, smem_raw);
+    select_smem(SLICES, K, &s, smem_raw);
     const int rank = (int)cluster.block_rank(), entry = blockIdx.x / SLICES;
     const int lo = (int)((long long)p.vocab * rank / SLICES), hi = (int)((long long)p.vocab * (rank + 1) / SLICES);
     const size_t row0 = (size_t)entry * K;
@@ -241,7 +240,7 @@ beam_select_kernel(SelectParams p)
             asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
             // The bound, one that K threads' largest logits reach.  Up to four beams the smallest of four maxima (of a quarter of the threads; 8 logits
             // reach it on average, 50 once in a million), up to eight the smallest of four second largest, of eight maxima each (14; one by one, the
-            // K-th largest of 32 took 32.5 us where this takes 28.9), else a value that K to 5 K / 4 of 64 maxima reach, by bisection.  The two
+            // K-th largest of 32 took 32.5 us where this took 28.9), else a value that K to 5 K / 4 of 64 maxima reach, by bisection.  The two
             // buffers in turn: who writes one again has passed the barrier behind everybody's reading of it.
             uint32_t left = s_maxima[group][buffer][lane];
             if (K <= 4) {
@@ -377,8 +376,9 @@ beam_select_kernel(SelectParams p)
             }
             return Choice{0ull, 0};
         };
-        const int n = K <= 4 ? join_lists<1>(K, score_of, s_chosen, s_chosen_pair) : K <= 8 ? join_lists<2>(K, score_of, s_chosen, s_chosen_pair)
-                    : K <= 16 ? join_lists<4>(K, score_of, s_chosen, s_chosen_pair) : join_lists<8>(K, score_of, s_chosen, s_chosen_pair);
+        const int lists = K * SLICES;
+        const int n = lists <= 32 ? join_lists<1>(K, lists, score_of, s_chosen, s_chosen_pair) : lists <= 64 ? join_lists<2>(K, lists, score_of, s_chosen, s_chosen_pair)
+                    : lists <= 128 ? join_lists<4>(K, lists, score_of, s_chosen, s_chosen_pair) : join_lists<8>(K, lists, score_of, s_chosen, s_chosen_pair);
         if (lane == 0) s_found = n;
     }
     __syncthreads();
@@ -404,39 +404,44 @@ beam_select_kernel(SelectParams p)
     }
 }
 
-template <int THREADS, int PT>
+template <int SLICES, int THREADS, int PT>
 amq_status launch_select_as(const SelectParams& p, int batch, int groups, cudaStream_t st)
 {
-    const size_t smem = select_smem(p.beams, nullptr, nullptr);
-    auto kernel = beam_select_kernel<THREADS, PT>;
+    const size_t smem = select_smem(SLICES, p.beams, nullptr, nullptr);
+    auto kernel = beam_select_kernel<SLICES, THREADS, PT>;
     AMQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     AMQ_CUDA_TRY(launch_kernel(kernel, dim3((unsigned)(batch * SLICES)), dim3((unsigned)(THREADS * groups)), smem, st, true, p));
     AMQ_LAUNCH_CHECK();
     return AMQ_OK;
 }
 
-template <int THREADS>
+// MOST: words of a thread and piece
+template <int SLICES, int THREADS, int MOST>
 amq_status launch_select_groups(const SelectParams& p, int batch, int groups, cudaStream_t st)
 {
     if (groups > p.beams) groups = p.beams;
-    const int slice = (p.vocab + SLICES - 1) / SLICES, most = groups == 1 ? 24 : 12;
-    const int pieces = (slice + THREADS * most - 1) / (THREADS * most), words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
-    if (words <= 2) return launch_select_as<THREADS, 2>(p, batch, groups, st);
-    if (words <= 5) return launch_select_as<THREADS, 5>(p, batch, groups, st);
-    if (words <= 8) return launch_select_as<THREADS, 8>(p, batch, groups, st);
-    if (words <= 10) return launch_select_as<THREADS, 10>(p, batch, groups, st);
-    if (words <= 12) return launch_select_as<THREADS, 12>(p, batch, groups, st);
-    if (words <= 16) return launch_select_as<THREADS, 16>(p, batch, groups, st);
-    if (words <= 21) return launch_select_as<THREADS, 21>(p, batch, groups, st);
-    return launch_select_as<THREADS, 24>(p, batch, groups, st);
+    const int slice = (p.vocab + SLICES - 1) / SLICES;
+    const int pieces = (slice + THREADS * MOST - 1) / (THREADS * MOST), words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
+    if (words <= 2) return launch_select_as<SLICES, THREADS, 2>(p, batch, groups, st);
+    if (words <= 5) return launch_select_as<SLICES, THREADS, 5>(p, batch, groups, st);
+    if (words <= 8) return launch_select_as<SLICES, THREADS, 8>(p, batch, groups, st);
+    if (words <= 10) return launch_select_as<SLICES, THREADS, 10>(p, batch, groups, st);
+    if constexpr (MOST > 12) {
+        if (words > 21) return launch_select_as<SLICES, THREADS, 24>(p, batch, groups, st);
+        if (words > 16) return launch_select_as<SLICES, THREADS, 21>(p, batch, groups, st);
+        if (words > 12) return launch_select_as<SLICES, THREADS, 16>(p, batch, groups, st);
+    }
+    return launch_select_as<SLICES, THREADS, 12>(p, batch, groups, st);
 }
 
 amq_status launch_select(const SelectParams& p, int batch, cudaStream_t st)
 {
-    // Beams at a time: as many as leave the CTAs of all entries on the GPU at once.  Beyond 16 the lists' memory leaves an SM few CTAs, and four beams at a time
-    // make up for that (64 entries, 32 beams, 9999 tokens: 134 us, 257 with one).
-    if (batch * SLICES <= 148) return p.beams > 4 ? launch_select_groups<128>(p, batch, 8, st) : launch_select_groups<256>(p, batch, 4, st);
-    return launch_select_groups<256>(p, batch, p.beams > 16 ? 4 : batch * SLICES <= 296 ? 2 : 1, st);
+    // Few entries: eight CTAs of all the threads an SM allows, as long as the GPU holds the clusters at once (14 of eight CTAs, 33 of four; a few SMs of every
+    // GPC are left over).  Then four CTAs an entry, with as many beams at a time as leave those of all entries on the GPU at once; for many beams, whose lists
+    // leave an SM few CTAs, two at least.  By eight and by four CTAs, 8 beams of 9999: 14 entries 9.7 and 10.5 us, 16 13.6 and 10.5; four, two and one
+    // beam at a time: 32 entries 11.0, 12.2 and 16.3, 60 20.1, 14.3 and 17.6, 90 27, 22.8 and 19.4; with 16 beams 51, 45.6 and 41.6, of 42000 90, 90 and 105.
+    if (batch <= 14) return p.beams > 4 ? launch_select_groups<8, 128, 12>(p, batch, 8, st) : launch_select_groups<8, 256, 12>(p, batch, 4, st);
+    return launch_select_groups<4, 256, 24>(p, batch, batch <= 33 ? 4 : batch <= 66 || p.beams > 8 ? 2 : 1, st);
 }
 
 // ---- reordering ------------------------------------------------------------------------------------------------------
@@ -523,7 +528,7 @@ amq_status amq_beam_select(const float* logits, int ld, int vocab, const float* 
                            float* scores_out, int32_t* parents, int32_t* tokens, int32_t* finished_out, void* stream)
 {
     if (vocab < 1 || ld < vocab || batch < 0 || beams < 1 || eos < -1 || eos >= vocab || (finished && eos < 0)) return AMQ_ERR_INVALID_ARG;
-    if (beams > AMQ_MAX_BEAMS || (long long)beams * vocab > 0x7ffffffell || (long long)batch * amq::SLICES > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
+    if (beams > AMQ_MAX_BEAMS || (long long)beams * vocab > 0x7ffffffell || 8ll * batch > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
     if (batch == 0) return AMQ_OK;
     if (!logits || !scores || !scores_out || !parents || !tokens) return AMQ_ERR_INVALID_ARG;
     amq::SelectParams p{logits, ld, vocab, scores, finished, eos, beams, scores_out, parents, tokens, finished_out};

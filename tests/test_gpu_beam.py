@@ -46,7 +46,8 @@ def same(got, want):
 
 
 @pytest.mark.parametrize("batch,beams,vocab", [(1, 1, 1), (1, 4, 1), (2, 3, 5), (1, 5, 9999), (3, 8, 42000), (7, 2, 100), (20, 10, 2047), (2, 16, 20001),
-                                               (1, 32, 50000), (300, 4, 333), (2, 32, 31), (1, 1, 200000), (5, 7, 2049)])
+                                               (1, 32, 50000), (300, 4, 333), (2, 32, 31), (1, 1, 200000), (5, 7, 2049),
+                                               (14, 5, 700), (15, 5, 700), (33, 8, 9000), (34, 8, 9000), (66, 4, 26000), (67, 4, 26000), (67, 9, 3), (70, 32, 2000)])
 def test_choice(amq, batch, beams, vocab):
     gen = torch.Generator(device="cuda").manual_seed(batch + beams + vocab)
     logits = torch.randn((batch * beams, vocab), device="cuda", generator=gen) * 2.5
