@@ -12,8 +12,8 @@
 // sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the share's K-th largest logit comes from the maxima of 32 or 64 groups
 // of threads, and little more than K logits reach it; those are written down, sorted by a warp, and go to the first CTA's shared memory, which
 // joins them by score.
-// Bound by instructions, 22 for a lane and logit at 21 logits a thread and row: the exponentials' four and the comparisons, and some 300 a warp and
-// row for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.5 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
+// Bound by instructions and barriers, 16 instructions for a lane and logit at 21 logits a thread and piece: load, maximum, exponential, sum, and some 240 a warp and
+// piece for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.5 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
 // one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 9 us, a chain of two barriers, the cluster's exchange and the join.
 #include <cooperative_groups.h>
 
