@@ -86,6 +86,7 @@ CASES = [  # lengths, page size, heads, group, d, k, q_len
     # sequences without tokens between others, more than a warp of them; more blocks than CTAs fit the GPU
     ([0, 0, 700, 0, 1, 0, 900] + [0] * 40 + [33, 0, 64] * 10 + [0, 5], 16, 2, 4, 64, 4, 1), ([600, 40], 16, 16, 4, 128, 2, 40),
     ([0] * 70 + [2000], 32, 1, 8, 128, 1, 1), ([513] * 40, 1, 4, 1, 128, 4, 1),
+    ([1500, 3, 0, 2040] + [70] * 60, 16, 16, 1, 64, 2, 1), ([1025, 2048, 1, 31] * 4, 16, 64, 2, 40, 1, 2),
 ]
 
 
