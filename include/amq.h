@@ -360,8 +360,8 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  * t < lengths[b] - q_len + 1 + i (causal), those on no page left out; q_heads is a multiple of heads, and query head h reads the
  * keys and values of head h / (q_heads / heads):
  *   s[t] = scale * (q . khat[t]),  p = softmax(s),  out = sum_t p[t] vhat[t],  khat and vhat the values that the planes stand for.
- * A query that sees no token gets zeros; one that holds NaN or infinities, or sees a coefficient that is NaN or infinite, gets NaN.  What no query sees
- * is not looked at, whatever it holds.
+ * A query that sees no token gets zeros; one that holds NaN or infinities, or sees a coefficient that is NaN or infinite, gets NaN.  What a query
+ * does not see does not change its result, whatever it holds.
  *   q   fp32, element (b, i, h, j) at q[b * q_batch + i * q_token + h * q_head + j] (strides in elements).
  *   out [batch][q_len][q_heads][d] fp32.
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
@@ -402,8 +402,8 @@ AMQ_API amq_status amq_beam_select(const float* logits, int ld, int vocab, const
  * The states behind the chosen beams: for `count` states (h, c, token histories, rows of a block table, ..) and every entry e, beam b
  *   dst[i] row (e * beams + b) = src[i] row (e * beams + parents[e][b]),
  * rows of row_bytes[i] bytes at strides of src_stride[i] and dst_stride[i] bytes (all multiples of 4, addresses too: AMQ_ERR_ALIGNMENT).  dst[i]
- * may be src[i] with the same stride (in place); it may not overlap any source otherwise, nor any other dst (AMQ_ERR_INVALID_ARG where the addresses are equal).  Parents outside [0, beams) are clamped.  Bytes of
- * dst between the rows are left as they were.
+ * may be src[i] with the same stride (in place); it may not overlap any source otherwise, nor any other dst (AMQ_ERR_INVALID_ARG where the
+ * addresses are equal).  Parents outside [0, beams) are clamped.  Bytes of dst between the rows are left as they were.
  * src, dst, row_bytes, src_stride and dst_stride are HOST arrays of `count` <= AMQ_MAX_STATES; what src and dst hold are DEVICE pointers.
  */
 #define AMQ_MAX_STATES 8

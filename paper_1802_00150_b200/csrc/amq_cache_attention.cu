@@ -698,8 +698,8 @@ struct AttentionPlan { int rows, row_tiles, row_blocks, warps, shares; long long
 // Sequences of 1024 tokens, 8 heads, 4 query heads each, whole and in shares: one 16.5 and 17.2 us, 16 17.4 and 22.5, 64 48 and 57, 256 151 and 180;
 // of 2048: 8 28.7 and 23, 32 of 512 to 2048 48 and 42.  Up to 2048 tokens whole too where the CTAs are many, so that the GPU evens them out: 256 sequences of up
 // to 200 tokens 39 and 67 us, of 1 to 2048 118 and 140 (most of them short) or 177 and 181 (of any length alike), of 2048 279 and 313; three of 2048 among
-// 125 short ones are slower, 61 and 53, and with longer ones that grows (8192: 183 and 65).  64 sequences of 1024 to 4096 tokens in equal numbers of shares each took 127 us, dealt out
-// 112; one of 65000 tokens 94 and 79.
+// 125 short ones are slower, 61 and 53, and with longer ones that grows (8192: 183 and 65).  64 sequences of 1024 to 4096 tokens in equal numbers of
+// shares each took 127 us, dealt out 112; one of 65000 tokens 94 and 79.
 // Two row tiles to a CTA where rows fill them: 8 rows over 65000 tokens 79 us, 85 with one; 9 rows over 20 x 1500 tokens (3 bits) 47 us, 37 with one.
 AttentionPlan attention_plan(int batch, int q_len, int q_heads, int heads, long long max_tokens)
 {
