@@ -367,7 +367,7 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
  *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
  * Products with the planes are exact, on q and on p times coefficients held as 31-bit fixed-point numbers (relative to a query's largest element, and
- * to the largest weight and coefficient among 32 tokens; elements of a query below 2^-98 lose bits); everything else is fp32.  Results repeat
+ * to the largest weight and coefficient among those of 32 tokens that it sees; elements of a query below 2^-98 lose bits); everything else is fp32.  Results repeat
  * bit for bit for the same sizes and lengths.
  */
 AMQ_API size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens);

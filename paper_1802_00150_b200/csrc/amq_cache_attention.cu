@@ -395,7 +395,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 
         // The coefficients by planes, so that those of tokens 2 c, 2 c + 1 lie together; the values' largest decides the fixed point of the tile's
         // weights.  (The barrier behind the copies lies behind everybody's reading of the last tile's.)
-        uint32_t largest = 0, largest_k = 0;
+        uint32_t mine = 0, mine_k = 0;          // of this lane's token
         float va[K];
         float ka[K];
         load_row<K>(st.ka + lane * pitch(K), ka);
@@ -403,19 +403,19 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             coef.k[i][lane] = ka[i];
-            largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
-            largest_k = max(largest_k, __float_as_uint(ka[i]) & 0x7fffffffu);
+            mine = max(mine, __float_as_uint(va[i]) & 0x7fffffffu);
+            mine_k = max(mine_k, __float_as_uint(ka[i]) & 0x7fffffffu);
         }
-        largest = __reduce_max_sync(0xffffffffu, largest_k >= 0x7f800000u ? largest_k : largest);
+        uint32_t largest = __reduce_max_sync(0xffffffffu, mine_k >= 0x7f800000u ? mine_k : mine);
         if (largest >= 0x7f800000u) {           // NaN or infinite coefficients: they count for the rows that see them, and for those only
-            bool bad = largest_k >= 0x7f800000u;
-            largest = 0;
+            bool bad = mine_k >= 0x7f800000u;
+            mine = 0;
 #pragma unroll
             for (int i = 0; i < K; ++i) {
                 if (!isfinite(va[i])) { bad = true; va[i] = 0.0f; }
-                largest = max(largest, __float_as_uint(va[i]) & 0x7fffffffu);
+                mine = max(mine, __float_as_uint(va[i]) & 0x7fffffffu);
             }
-            largest = __reduce_max_sync(0xffffffffu, largest);
+            largest = __reduce_max_sync(0xffffffffu, mine);
             const uint32_t all_bad = __ballot_sync(0xffffffffu, bad);
 #pragma unroll
             for (int z = 0; z < MT; ++z)
@@ -423,9 +423,25 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
         }
 #pragma unroll
         for (int i = 0; i < K; ++i) coef.v[i][lane] = va[i];
+        // Where rows of the block see different tokens (the last tiles of a call with several queries a sequence), each goes by the largest of those that it
+        // sees: a later query's token would take bits from the earlier ones' weights.
+        uint32_t size[MT];
+        bool differ = false;
+#pragma unroll
+        for (int z = 0; z < MT; ++z) { size[z] = largest; differ |= seen[z] != on_a_page; }
+        if (__any_sync(0xffffffffu, differ)) {
+#pragma unroll
+            for (int z = 0; z < MT; ++z)
+#pragma unroll
+                for (int row = 0; row < ROWS; ++row) {
+                    const uint32_t tokens = __shfl_sync(0xffffffffu, seen[z], 4 * row), of_row = __reduce_max_sync(0xffffffffu, tokens >> lane & 1 ? mine : 0u);
+                    if (r == row) size[z] = of_row;
+                }
+        }
         __syncwarp();
-        const int ev = max((int)(largest >> 23), 30);
-        const float to_fixed = __int_as_float((283 - ev) << 23), from_fixed = __int_as_float((ev - 29) << 23);       // products below 2^30
+        float to_fixed[MT];                     // products below 2^30
+#pragma unroll
+        for (int z = 0; z < MT; ++z) to_fixed[z] = __int_as_float((283 - max((int)(size[z] >> 23), 30)) << 23);
 
         // scores of tokens 8 n + 2 c, 8 n + 2 c + 1
         float s[MT][4][2];
@@ -512,7 +528,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             for (int n = 0; n < 4; ++n) {
                 const float e0 = exp2_approx(s[z][n][0] - ref), e1 = exp2_approx(s[z][n][1] - ref);
                 sum += e0 + e1;
-                const f32x2 ws = mul2(pack2(e0, e1), pack2(to_fixed, to_fixed));
+                const f32x2 ws = mul2(pack2(e0, e1), pack2(to_fixed[z], to_fixed[z]));
 #pragma unroll
                 for (int i = 0; i < K; ++i) {
                     float f0, f1;
@@ -534,7 +550,7 @@ cache_attention_kernel(const __grid_constant__ AttentionParams p)
             mma_s8u8(ones, ap[z][0], 0x01010101u, 0x01010101u, start);
 #pragma unroll
             for (int q = 1; q < K; ++q) mma_s8u8(ones, ap[z][q], 0x01010101u, 0x01010101u);
-            unit[z] = tile_factor * from_fixed * w1;                // (w0 = 2^16 w1)
+            unit[z] = tile_factor * __int_as_float(0x7f000000 - __float_as_int(to_fixed[z])) * w1;         // (1 / to_fixed, a power of two; w0 = 2^16 w1)
             const float base = -unit[z] * fmaf(65536.0f, __int_as_float(ones[0]) - MAGIC, __int_as_float(ones[2]) - MAGIC);
             base_2[z] = pack2(base, base); corr_2[z] = pack2(corr, corr);
         }
