@@ -172,17 +172,17 @@ beam_select_kernel(SelectParams p)
     constexpr bool AHEAD = PT <= 12;    // a second piece in registers, fetched while one is worked on; with longer ones the SM's other CTAs have to do
     float cur[PT], nxt[AHEAD ? PT : 1];
     auto load = [&](float (&v)[PT], int b, int c) {
-        const int first = lo + c * CHUNK + at_group;
-        const float* z = p.logits + (row0 + b) * p.ld + first;
-        if (lo + (c + 1) * CHUNK <= hi) {
+        const int left = hi - lo - c * CHUNK;       // words from this piece on (a place behind the share may lie behind 2^31; what is left never does)
+        const float* z = p.logits + (row0 + b) * p.ld + (size_t)(lo + c * CHUNK) + at_group;
+        if (left >= CHUNK) {
 #pragma unroll
             for (int i = 0; i < PT; ++i) v[i] = __ldcg(z + i * THREADS);
-        } else if (lo + c * CHUNK + SURE * THREADS <= hi) {         // (a row's only piece, as a rule: its first words need no comparison)
+        } else if (left >= SURE * THREADS) {        // (a row's only piece, as a rule: its first words need no comparison)
 #pragma unroll
-            for (int i = 0; i < PT; ++i) v[i] = i < SURE || first + i * THREADS < hi ? __ldcg(z + i * THREADS) : -INFINITY;
+            for (int i = 0; i < PT; ++i) v[i] = i < SURE || at_group + i * THREADS < left ? __ldcg(z + i * THREADS) : -INFINITY;
         } else {
 #pragma unroll
-            for (int i = 0; i < PT; ++i) v[i] = first + i * THREADS < hi ? __ldcg(z + i * THREADS) : -INFINITY;
+            for (int i = 0; i < PT; ++i) v[i] = at_group + i * THREADS < left ? __ldcg(z + i * THREADS) : -INFINITY;
         }
     };
     if (chunks && group < K) load(cur, group, 0);           // (whether it counts is not known yet)
@@ -318,16 +318,16 @@ beam_select_kernel(SelectParams p)
             for (int i = lane; i - lane < n; i += 32) kept = best_of(kept, i < n ? list[i] : 0ull);
             if (lane < K) best[lane] = kept;
         } else {                        // more ties than the list holds: the slice once more, past the best so far, a place of which each lane keeps
-            const float* z = p.logits + (row0 + q) * p.ld;
+            const float* z = p.logits + (row0 + q) * p.ld + lo;
             const uint32_t least = s_bound[q];
             unsigned long long kept = 0;
-            for (int t0 = lo; t0 < hi; t0 += 128) {
+            for (int t0 = 0; t0 < hi - lo; t0 += 128) {             // (a share is a quarter of the vocabulary at most)
                 float x[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = t0 + 32 * i + lane < hi ? __ldcg(z + t0 + 32 * i + lane) : -INFINITY;
+                for (int i = 0; i < 4; ++i) x[i] = t0 + 32 * i + lane < hi - lo ? __ldcg(z + t0 + 32 * i + lane) : -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const unsigned long long k = x[i] > -INFINITY && ordered(x[i]) >= least ? candidate(x[i], t0 + 32 * i + lane) : 0ull;
+                    const unsigned long long k = x[i] > -INFINITY && ordered(x[i]) >= least ? candidate(x[i], lo + t0 + 32 * i + lane) : 0ull;
                     uint32_t above = __ballot_sync(0xffffffffu, k > __shfl_sync(0xffffffffu, kept, K - 1));
                     for (; above; above &= above - 1) {
                         const unsigned long long one = __shfl_sync(0xffffffffu, k, __ffs(above) - 1), up = __shfl_up_sync(0xffffffffu, kept, 1);
@@ -420,7 +420,7 @@ template <int SLICES, int THREADS, int MOST>
 amq_status launch_select_groups(const SelectParams& p, int batch, int groups, cudaStream_t st)
 {
     if (groups > p.beams) groups = p.beams;
-    const int slice = (p.vocab + SLICES - 1) / SLICES;
+    const int slice = (p.vocab - 1) / SLICES + 1;
     const int pieces = (slice + THREADS * MOST - 1) / (THREADS * MOST), words = ((slice + pieces - 1) / pieces + THREADS - 1) / THREADS;
     if (words <= 2) return launch_select_as<SLICES, THREADS, 2>(p, batch, groups, st);
     if (words <= 5) return launch_select_as<SLICES, THREADS, 5>(p, batch, groups, st);
