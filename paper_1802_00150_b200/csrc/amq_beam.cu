@@ -18,6 +18,7 @@
 #include <cooperative_groups.h>
 
 #include "amq_common.cuh"
+#include "amq_pairs.cuh"
 
 namespace amq {
 namespace {
@@ -49,9 +50,10 @@ __device__ __forceinline__ unsigned long long candidate(float v, int token) { re
 __device__ __forceinline__ float exp2_ftz(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 constexpr float LOG2E = 1.44269504f;
 
-// Sums of exp(z) as s 2^m, m = the largest logit times LOG2E, rounded: the exponents z LOG2E - m are one rounding each, and m / LOG2E in double takes
-// the roundings of m and of the constant back (what is left of them is 1e-8 (z - max)).
+// Sums of exp(z) as s exp(m), m = the largest logit: the exponents (z - m) LOG2E are two roundings each, relative to themselves, and no finite logit is too
+// large for them (m LOG2E is, from 2.4e38 on).
 struct WarpSum { float m, s; };
+__device__ __forceinline__ float exp_from(float z, float m) { return exp2_ftz((z - m) * LOG2E); }
 
 // shared memory of a CTA.  What the others send lies in the first CTA's.
 struct SelectSmem {
@@ -152,7 +154,7 @@ beam_select_kernel(SelectParams p)
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ float s_score[AMQ_MAX_BEAMS];
     __shared__ int s_done[AMQ_MAX_BEAMS];
-    __shared__ double s_lse[AMQ_MAX_BEAMS];
+    __shared__ float s_top[AMQ_MAX_BEAMS]; __shared__ double s_log[AMQ_MAX_BEAMS];       // a row's largest logit, and the logarithm of its sum relative to that
     __shared__ uint32_t s_maxima[MAX_GROUPS][2][MAXIMA];
     __shared__ int s_count[AMQ_MAX_BEAMS]; __shared__ uint32_t s_bound[AMQ_MAX_BEAMS];
     __shared__ int s_found;
@@ -231,10 +233,19 @@ beam_select_kernel(SelectParams p)
                 s_maxima[group][buffer][at_group / (THREADS / 64)] = of_some;
             }
         }
-        const float m_new = fmaxf(m, top * LOG2E), ref = m_new == -INFINITY ? 0.0f : m_new;
-        sum *= exp2_ftz(m - ref);
+        const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.0f : m_new;
+        sum *= exp_from(m, ref);
+        {
+            const f32x2 less = pack2(-ref, -ref), scale = pack2(LOG2E, LOG2E);
 #pragma unroll
-        for (int i = 0; i < PT; ++i) sum += exp2_ftz(fmaf(now[i], LOG2E, -ref));
+            for (int i = 0; i + 1 < PT; i += 2) {
+                float e0, e1;
+                unpack2(mul2(add2(pack2(now[i], now[i + 1]), less), scale), e0, e1);
+                sum += exp2_ftz(e0);
+                sum += exp2_ftz(e1);
+            }
+            if (PT & 1) sum += exp_from(now[PT - 1], ref);
+        }
         m = m_new;
         if (c != 1) {
             asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(THREADS) : "memory");
@@ -286,7 +297,7 @@ beam_select_kernel(SelectParams p)
         if (nb != b) {                  // the row is through: the warp's share of its sum
             const uint32_t wm = redux_max(m > -INFINITY ? ordered(m) : 0u);
             const float M = wm ? from_ordered(wm) : -INFINITY;
-            float t = sum * exp2_ftz(m - (wm ? M : 0.0f));        // (nothing but -inf: 0)
+            float t = sum * exp_from(m, wm ? M : 0.0f);           // (nothing but -inf: 0)
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
             if (lane == 0) sums_there[b * SLICES * WARPS + warp] = {M, t};
@@ -356,10 +367,10 @@ beam_select_kernel(SelectParams p)
         for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
         double t = isfinite(M) ? 0.0 : (double)NAN;
 #pragma unroll
-        for (int x = 0; x < SHARES; ++x) t += (double)(w[x].s * exp2f(w[x].m - M));
+        for (int x = 0; x < SHARES; ++x) t += (double)(w[x].s * exp2f((w[x].m - M) * LOG2E));
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
-        if (lane == 0) s_lse[q] = (double)M / (double)LOG2E + log(t);
+        if (lane == 0) { s_top[q] = M; s_log[q] = log(t); }
     }
     __syncthreads();
     if (tid < 32) {
@@ -368,9 +379,9 @@ beam_select_kernel(SelectParams p)
             const int q = list / SLICES;
             if (open(q)) {
                 const unsigned long long k = s.best[(size_t)list * K + place];
-                const double lse = s_lse[q];
-                if (k && isfinite(lse))
-                    return Choice{ordered((double)s_score[q] + ((double)from_ordered((uint32_t)(k >> 32)) - lse)), q * p.vocab + (int)~(uint32_t)k};
+                const double log_sum = s_log[q];
+                if (k && isfinite(log_sum))
+                    return Choice{ordered((double)s_score[q] + ((double)from_ordered((uint32_t)(k >> 32)) - (double)s_top[q] - log_sum)), q * p.vocab + (int)~(uint32_t)k};
             } else if (s_done[q] && list % SLICES == 0 && place == 0 && isfinite(s_score[q])) {
                 return Choice{ordered((double)s_score[q]), q * p.vocab + p.eos};
             }

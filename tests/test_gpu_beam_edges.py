@@ -1,4 +1,4 @@
-"""Beam search's choice at the ends of what it accepts: vocabularies up to 2^31."""
+"""Beam search's choice at the ends of what it accepts: logits at the ends of fp32, vocabularies up to 2^31."""
 import math
 
 import pytest
@@ -36,3 +36,42 @@ def test_the_largest_vocabulary(amq):  # noqa: F811
     logits[most - 1000:] = 9.0
     got, _, tokens, _ = amq.beam_select(logits.view(1, most), torch.zeros((1, 1), device="cuda"))
     assert tokens.item() == most - 1000
+
+
+LOWEST = torch.finfo(torch.float32).min
+
+
+@pytest.mark.parametrize("batch,vocab", [(1, 7), (1, 9999), (20, 3001), (70, 20000)])
+def test_logits_at_the_ends_of_fp32(amq, batch, vocab):  # noqa: F811
+    """Finite logits of any size have a log-sum-exp: rows of the type's lowest value alone (every token masked with it), of values whose product with log2(e) is
+    beyond fp32, with a few such values among others.  Against the definition in double, summed relative to the row's largest."""
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    beams = 6
+    z = torch.randn((batch, beams, vocab), device="cuda", generator=gen) * 2.5
+    scores = -20 * torch.rand((batch, beams), device="cuda", generator=gen)
+    z[:, 1] = LOWEST                                        # -log(vocab) each
+    z[:, 2] = -3e38
+    z[:, 2, 5] = LOWEST                                     # (nothing beside the others)
+    z[:, 3, 3] = 3e38                                       # the one continuation with a probability
+    z[:, 4] = LOWEST
+    z[:, 4, 6] = 2.5e38
+    z[:, 4, 2] = 2.5e38                                     # two of them
+    z[:, 5, ::2] = LOWEST                                   # an ordinary mask
+    scores[:, 1] = -0.5 + math.log(vocab)                   # (so that the first tokens of the row are chosen)
+    scores[:, 2] = -0.6 + math.log(vocab)
+    d = z.double()
+    top = d.amax(2, keepdim=True)
+    total = scores.double()[..., None] + (d - top - torch.log(torch.exp(d - top).sum(2, keepdim=True)))
+    # (a library's sum over a row of equal numbers is off by 1e-15; far below what other candidates differ by)
+    total = (total.view(batch, -1).clamp(min=-1e20) * 1e10).round() / 1e10
+    best, at = torch.sort(total, dim=1, descending=True, stable=True)
+    got, parents, tokens, _ = amq.beam_select(z.view(batch * beams, vocab), scores)
+    assert torch.equal(parents.long(), at[:, :beams] // vocab) and torch.equal(tokens.long(), at[:, :beams] % vocab)
+    assert ((got.double() - best[:, :beams]).abs() <= 2.0 ** -24 * best[:, :beams].abs() + 3e-6).all()
+
+
+def test_a_single_beam_of_lowest_values(amq):  # noqa: F811
+    """A uniform row, whatever its value: the first token, at -log(vocab)."""
+    for value in (LOWEST, -1.0, 0.0, 3.4e38):
+        got, parents, tokens, _ = amq.beam_select(torch.full((1, 4096), value, device="cuda"), torch.zeros((1, 1), device="cuda"))
+        assert parents.item() == 0 and tokens.item() == 0 and abs(got.item() + math.log(4096)) <= 2.0 ** -20
