@@ -381,7 +381,8 @@ AMQ_API amq_status amq_cache_attention(const float* q, long long q_batch, long l
  * Beam search on the output layer of Eq. 6 (the paper decodes greedily; `beams` = 1 is that): for each of `batch` entries the `beams` best of all
  * beams * vocab continuations,
  *   score(b, t) = scores[b] + logits[b][t] - log(sum_u exp(logits[b][u])),
- * best first, equal scores by the smaller b * vocab + t.  Candidates are compared unrounded (in double); scores_out is rounded to fp32.
+ * best first, equal scores by the smaller b * vocab + t.  Scores are computed and compared in double, and one beam's continuations rank as their logits do
+ * (which a score of -1e9 may not tell apart); scores_out is rounded to fp32.
  *   logits       rows entry * beams + b of `ld` >= vocab floats; -inf takes a token out.
  *   scores       [batch][beams] fp32.  A beam whose score is not finite, or whose logits hold NaN or +inf or nothing but -inf, has no
  *                continuation: all its pairs score -inf, as do the tokens taken out.  Pairs of -inf are chosen only where there are no others, the

@@ -2,9 +2,9 @@
 // of the states that belong to the chosen beams.
 //
 // Choice.  score(b, t) = score_b + z_bt - log sum_u exp(z_bu); the `beams` best of all (beam, token) pairs, in the order (score descending, pair
-// index ascending).  Within a row the order is that of the logits, so one pass over the logits finds each row's largest and the sum of its
-// exponentials together, and only beams x 8 x beams candidates are compared by score, in double: candidates of two beams may lie closer
-// than fp32 rounding of a score of -20 (2e-6), those of one beam never change places.
+// index ascending).  Within a row the order is that of the logits (also where different logits round to one score), so one pass over the logits finds each
+// row's largest and the sum of its exponentials together, and only beams x 8 x beams candidates are compared by score, in double: candidates
+// of two beams may lie closer than fp32 rounding of a score of -20 (2e-6).
 //
 // A cluster of eight or four CTAs takes a batch entry; CTA c reads the share c of every beam's row, so any number of beams is balanced, and one entry
 // alone still has eight SMs.  A group of 128 or 256 threads takes a beam's share in pieces of up to 24 words a thread, with up to twelve the next piece on its
@@ -16,6 +16,8 @@
 // piece for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.5 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
 // one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 9 us, a chain of two barriers, the cluster's exchange and the join.
 #include <cooperative_groups.h>
+
+#include <type_traits>
 
 #include "amq_common.cuh"
 #include "amq_pairs.cuh"
@@ -110,11 +112,13 @@ __device__ __forceinline__ unsigned long long best_of(unsigned long long kept, u
 
 struct Choice { unsigned long long score; int pair; };       // score 0: none
 
-// One warp joins the sorted lists (one for each beam and slice): LISTS of them a lane, and beam after beam of the result the best of their heads,
-// by score, then pair.  `score_of(list, place)`.  Returns how many there were; lane 0 has written them down.
-template <int LISTS, typename F>
-__device__ __forceinline__ int join_lists(int K, int lists, F&& score_of, double* chosen, int* chosen_pair)
+// One warp joins the sorted lists (one for each beam and slice, SLICES a beam): LISTS of them a lane, and beam after beam of the result the best of their heads: by
+// score; equal scores by beam, of one beam by logit (different logits may give one score, of a beam far below the others: a step of a double of -1e9 is 1e-7), then by
+// token.  `score_of(list, place)`, `logit_of(list, place)` in the order of integers.  Returns how many there were; lane 0 has written them down.
+template <int SLICES, int LISTS, typename F, typename G>
+__device__ __forceinline__ int join_lists(int K, int lists, F&& score_of, G&& logit_of, double* chosen, int* chosen_pair)
 {
+    static_assert(32 % SLICES == 0, "a lane's lists are of different beams, the first of them of the smallest");
     const int lane = threadIdx.x & 31;
     Choice head[LISTS];
     int place[LISTS];
@@ -128,14 +132,28 @@ __device__ __forceinline__ int join_lists(int K, int lists, F&& score_of, double
         int from = 0;
 #pragma unroll
         for (int x = 1; x < LISTS; ++x)
-            if (head[x].score > best.score || (head[x].score == best.score && head[x].pair < best.pair)) { best = head[x]; from = x; }
+            if (head[x].score > best.score) { best = head[x]; from = x; }
         const uint32_t hi = redux_max((uint32_t)(best.score >> 32));
         if (hi == 0u) return r;                     // (a finite score's high word is not 0)
         const uint32_t lo = redux_max((uint32_t)(best.score >> 32) == hi ? (uint32_t)best.score : 0u);
-        const bool top = best.score == (((unsigned long long)hi << 32) | lo);
-        const uint32_t pair = __reduce_min_sync(0xffffffffu, top ? (uint32_t)best.pair : 0xffffffffu);
-        if (lane == 0) { chosen[r] = from_ordered(((unsigned long long)hi << 32) | lo); chosen_pair[r] = (int)pair; }
-        if (top && (uint32_t)best.pair == pair) {   // (pairs are distinct: one lane)
+        uint32_t top = __ballot_sync(0xffffffffu, best.score == (((unsigned long long)hi << 32) | lo));
+        if (top & (top - 1)) {
+            auto among = [&](uint32_t v) {          // the lanes of `top` with the smallest value
+                const bool in = top >> lane & 1;
+                const uint32_t least = __reduce_min_sync(0xffffffffu, in ? v : 0xffffffffu);       // (all lanes, in front of any condition)
+                top = __ballot_sync(0xffffffffu, in && v == least);
+            };
+            among((uint32_t)((lane + 32 * from) / SLICES));
+            int at = place[0];
+#pragma unroll
+            for (int x = 1; x < LISTS; ++x) at = x == from ? place[x] : at;
+            among(top >> lane & 1 ? ~logit_of(lane + 32 * from, at) : 0xffffffffu);
+            among((uint32_t)best.pair);             // (pairs are distinct: one lane)
+        }
+        const int winner = __ffs(top) - 1;
+        const int pair = __shfl_sync(0xffffffffu, best.pair, winner);
+        if (lane == 0) { chosen[r] = from_ordered(((unsigned long long)hi << 32) | lo); chosen_pair[r] = pair; }
+        if (lane == winner) {
 #pragma unroll
             for (int x = 0; x < LISTS; ++x)
                 if (x == from) head[x] = ++place[x] < K ? score_of(lane + 32 * x, place[x]) : Choice{0ull, 0};
@@ -388,8 +406,10 @@ beam_select_kernel(SelectParams p)
             return Choice{0ull, 0};
         };
         const int lists = K * SLICES;
-        const int n = lists <= 32 ? join_lists<1>(K, lists, score_of, s_chosen, s_chosen_pair) : lists <= 64 ? join_lists<2>(K, lists, score_of, s_chosen, s_chosen_pair)
-                    : lists <= 128 ? join_lists<4>(K, lists, score_of, s_chosen, s_chosen_pair) : join_lists<8>(K, lists, score_of, s_chosen, s_chosen_pair);
+        auto logit_of = [&](int list, int place) { return (uint32_t)(s.best[(size_t)list * K + place] >> 32); };
+        auto join = [&](auto most) { return join_lists<SLICES, decltype(most)::value>(K, lists, score_of, logit_of, s_chosen, s_chosen_pair); };
+        const int n = lists <= 32 ? join(std::integral_constant<int, 1>{}) : lists <= 64 ? join(std::integral_constant<int, 2>{})
+                    : lists <= 128 ? join(std::integral_constant<int, 4>{}) : join(std::integral_constant<int, 8>{});
         if (lane == 0) s_found = n;
     }
     __syncthreads();

@@ -1,4 +1,5 @@
-"""Beam search's choice at the ends of what it accepts: logits at the ends of fp32, vocabularies up to 2^31."""
+"""Beam search's choice at the ends of what it accepts: logits at the ends of fp32, scores that do not tell
+logits apart, vocabularies up to 2^31."""
 import math
 
 import pytest
@@ -75,3 +76,39 @@ def test_a_single_beam_of_lowest_values(amq):  # noqa: F811
     for value in (LOWEST, -1.0, 0.0, 3.4e38):
         got, parents, tokens, _ = amq.beam_select(torch.full((1, 4096), value, device="cuda"), torch.zeros((1, 1), device="cuda"))
         assert parents.item() == 0 and tokens.item() == 0 and abs(got.item() + math.log(4096)) <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("batch", [1, 40])
+@pytest.mark.parametrize("score", [-1e9, -1e15, 0.0])
+def test_scores_that_do_not_tell_logits_apart(amq, batch, score):  # noqa: F811
+    """One beam's continuations rank as its logits do, equal ones by the smaller token, wherever in the row they lie, and beams of one score by the smaller
+    beam: logits a step of fp32 apart (6e-8) under a score whose double has steps of 1.2e-7, 0.125 or, for 0, steps that tell them apart."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    beams, vocab = 8, 6000
+    z = torch.zeros((batch, beams, vocab), device="cuda")
+    base = 0.75 * torch.ones(40, device="cuda")
+    steps = torch.randint(0, 9, (40,), device="cuda", generator=gen)        # (values again and again)
+    near = base + steps * 2.0 ** -24
+    for b in range(batch):
+        z[b, :, torch.randperm(vocab, device="cuda", generator=gen)[:40]] = near        # (all beams' rows alike)
+    scores = torch.full((batch, beams), score, device="cuda")
+    live = torch.arange(beams, device="cuda") < 2
+    scores[:, ~live] = -torch.inf
+    got, parents, tokens, _ = amq.beam_select(z.view(batch * beams, vocab), scores)
+    for b in range(batch):
+        row = z[b, 0].double()
+        order = torch.sort(row, descending=True, stable=True).indices[:beams].tolist()
+        if score == 0.0:                                    # the two beams' pairs of one logit side by side
+            place = {t: i for i, t in enumerate(order)}
+            want = sorted(((-row[t].item(), q, place[t], t) for q in range(2) for t in order))[:beams]
+            want = [(q, t) for _, q, _, t in want]
+        elif score == -1e15:                                # nothing but the beam's logits tells: the first beam's best
+            want = [(0, t) for t in order]
+        else:                                               # which logits share a score hangs on the log-sum-exp; the order of each beam's does not
+            chosen = list(zip(parents[b].tolist(), tokens[b].tolist()))
+            for q in range(2):
+                mine = [t for p, t in chosen if p == q]
+                assert mine == order[:len(mine)]
+            assert chosen[0] == (0, order[0]) and all(p < 2 for p, _ in chosen)
+            continue
+        assert list(zip(parents[b].tolist(), tokens[b].tolist())) == want
