@@ -382,7 +382,8 @@ AMQ_API amq_status amq_cache_attention(const float* q, long long q_batch, long l
  * beams * vocab continuations,
  *   score(b, t) = scores[b] + logits[b][t] - log(sum_u exp(logits[b][u])),
  * best first, equal scores by the smaller b * vocab + t.  Scores are computed and compared in double, and one beam's continuations rank as their logits do
- * (which a score of -1e9 may not tell apart); scores_out is rounded to fp32.
+ * (which a score of -1e9 may not tell apart); scores_out is rounded to fp32.  The logarithm is that of a sum of fp32 exponentials, within 2^-23 log(vocab) +
+ * 1.5e-6 of the exact one: continuations of two beams that lie so close may change places.
  *   logits       rows entry * beams + b of `ld` >= vocab floats; -inf takes a token out.
  *   scores       [batch][beams] fp32.  A beam whose score is not finite, or whose logits hold NaN or +inf or nothing but -inf, has no
  *                continuation: all its pairs score -inf, as do the tokens taken out.  Pairs of -inf are chosen only where there are no others, the

@@ -227,7 +227,8 @@ beam_select_kernel(SelectParams p)
 
     int b = chunks ? next_open(group) : K, c = 0, buffer = 0;
     if (b < K && b != group) load(cur, b, 0);
-    float m = -INFINITY, sum = 0.0f;
+    float m = -INFINITY;
+    double sum = 0.0;                   // (over pieces: in fp32 many equal terms of a long row would all be rounded one way, 4e-6 for 300000 tokens)
     uint32_t bound = 0, highest = 0;    // below every logit that counts; this thread's largest of the row so far
     // one piece, and the next one's loads
     auto step = [&](float (&now)[PT], auto& next) {
@@ -252,17 +253,18 @@ beam_select_kernel(SelectParams p)
             }
         }
         const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.0f : m_new;
-        sum *= exp_from(m, ref);
         {
+            float even = 0.0f, odd = 0.0f;          // of the piece, 12 words each
             const f32x2 less = pack2(-ref, -ref), scale = pack2(LOG2E, LOG2E);
 #pragma unroll
             for (int i = 0; i + 1 < PT; i += 2) {
                 float e0, e1;
                 unpack2(mul2(add2(pack2(now[i], now[i + 1]), less), scale), e0, e1);
-                sum += exp2_ftz(e0);
-                sum += exp2_ftz(e1);
+                even += exp2_ftz(e0);
+                odd += exp2_ftz(e1);
             }
-            if (PT & 1) sum += exp_from(now[PT - 1], ref);
+            if (PT & 1) even += exp_from(now[PT - 1], ref);
+            sum = fma(sum, (double)exp_from(m, ref), (double)(even + odd));
         }
         m = m_new;
         if (c != 1) {
@@ -315,12 +317,12 @@ beam_select_kernel(SelectParams p)
         if (nb != b) {                  // the row is through: the warp's share of its sum
             const uint32_t wm = redux_max(m > -INFINITY ? ordered(m) : 0u);
             const float M = wm ? from_ordered(wm) : -INFINITY;
-            float t = sum * exp_from(m, wm ? M : 0.0f);           // (nothing but -inf: 0)
+            float t = (float)sum * exp_from(m, wm ? M : 0.0f);           // (nothing but -inf: 0)
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
             if (lane == 0) sums_there[b * SLICES * WARPS + warp] = {M, t};
             if (at_group == 0) s_bound[b] = bound;
-            m = -INFINITY; sum = 0.0f; bound = 0; highest = 0;
+            m = -INFINITY; sum = 0.0; bound = 0; highest = 0;
         }
         b = nb; c = nc;
     };

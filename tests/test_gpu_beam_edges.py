@@ -112,3 +112,19 @@ def test_scores_that_do_not_tell_logits_apart(amq, batch, score):  # noqa: F811
             assert chosen[0] == (0, order[0]) and all(p < 2 for p, _ in chosen)
             continue
         assert list(zip(parents[b].tolist(), tokens[b].tolist())) == want
+
+
+@pytest.mark.parametrize("batch,beams,vocab", [(1, 8, 300000), (1, 1, 2000000), (16, 2, 300000), (1, 6, 9999)])
+def test_long_rows_of_equal_terms(amq, batch, beams, vocab):  # noqa: F811
+    """A few logits (one of 61, so that every thread meets some) above many equal ones, whose exponentials a running sum in fp32 would all round one way (4e-6 at 300000 tokens, 1.4e-5 at 2000000).  Here: an
+    exponential is within 2^-22 of itself, its exponent |d| off by 2^-23 |d| (two roundings); a piece's words are summed with 13 roundings, a warp's shares with six
+    and the store one: 20 2^-24.  The weighted mean of |d| is below log(vocab)."""
+    bound = 2.0 ** -22 + 2.0 ** -23 * math.log(vocab) + 20 * 2.0 ** -24
+    for d in torch.linspace(0.6, 8.2, 9).tolist():
+        logits = torch.full((batch * beams, vocab), 1.5 - d, device="cuda")
+        logits[:, ::61] = 1.5
+        got, _, tokens, _ = amq.beam_select(logits, torch.zeros((batch, beams), device="cuda"))
+        z = logits[0].double()
+        want = -(math.log(float(torch.exp(z - 1.5).sum())))
+        assert (tokens[:, 0] == 0).all()
+        assert (got[:, 0].double() - want).abs().max() <= bound + 2.0 ** -24 * abs(want)
