@@ -363,7 +363,7 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  * A query that sees no token gets zeros; one that holds NaN or infinities, or sees a coefficient that is NaN or infinite, gets NaN.  What a query
  * does not see does not change its result, whatever it holds.
  *   q   fp32, element (b, i, h, j) at q[b * q_batch + i * q_token + h * q_head + j] (strides in elements).
- *   out [batch][q_len][q_heads][d] fp32.
+ *   out [batch][q_len][q_heads][d] fp32; batch * q_len * q_heads up to AMQ_MAX_TOKENS (else AMQ_ERR_UNSUPPORTED, and a workspace of 0 bytes).
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
  *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
  * Products with the planes are exact, on q and on p times coefficients held as 31-bit fixed-point numbers (relative to a query's largest element, and

@@ -656,9 +656,10 @@ cache_attention_join_kernel(const __grid_constant__ AttentionParams p, int block
         if ((int)threadIdx.x < p.c.d) p.out[orow * p.c.d + threadIdx.x] = v;
     };
     const bool by_sequences = joins_by_sequences(p.batch, p.shares);
-    for (int b0 = at, step = by_sequences ? p.batch : p.shares - 1; b0 < p.batch; b0 += 32 * step) {
-        const int e = b0 + lane * step;
-        for (uint32_t empty = __ballot_sync(0xffffffffu, e < p.batch && tiles_of(p.c, e) == 0); empty; empty &= empty - 1) write(b0 + (__ffs(empty) - 1) * step, 0.0f);
+    const long long step = by_sequences ? p.batch : p.shares - 1;
+    for (long long b0 = at; b0 < p.batch; b0 += 32 * step) {
+        const long long e = b0 + lane * step;
+        for (uint32_t empty = __ballot_sync(0xffffffffu, e < p.batch && tiles_of(p.c, (int)e) == 0); empty; empty &= empty - 1) write((int)(b0 + (__ffs(empty) - 1) * step), 0.0f);
     }
     const long long total = total_tiles(p);
     const int shares = shares_of(p, total);
@@ -705,6 +706,13 @@ cache_attention_join_kernel(const __grid_constant__ AttentionParams p, int block
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     write(b, sum == 0.0f ? 0.0f : v / sum);
+}
+
+// all queries' rows in 31 bits, with room for a block behind the last
+bool rows_fit(int batch, int q_len, int q_heads)
+{
+    const long long queries = (long long)batch * q_len;
+    return queries <= AMQ_MAX_TOKENS && queries * q_heads <= AMQ_MAX_TOKENS;
 }
 
 struct AttentionPlan { int rows, row_tiles, row_blocks, warps, shares; long long blocks; size_t part_bytes, bytes; };
@@ -764,7 +772,7 @@ extern "C" {
 
 size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens)
 {
-    if (batch < 1 || q_len < 1 || q_heads < 1 || heads < 1 || q_heads % heads || d < 1 || d > AMQ_MAX_HEAD_DIM || max_tokens < 1) return 0;
+    if (batch < 1 || q_len < 1 || q_heads < 1 || heads < 1 || q_heads % heads || d < 1 || d > AMQ_MAX_HEAD_DIM || max_tokens < 1 || !amq::rows_fit(batch, q_len, q_heads)) return 0;
     return amq::attention_plan(batch, q_len, q_heads, heads, max_tokens).bytes;
 }
 
@@ -779,7 +787,7 @@ amq_status amq_cache_attention(const float* q, long long q_batch, long long q_to
                                    lengths, &p.c);
     if (s != AMQ_OK) return s;
     if (batch < 0 || q_len < 0 || q_heads < 1 || q_heads % heads) return AMQ_ERR_INVALID_ARG;
-    if ((long long)batch * q_len * q_heads > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
+    if (!amq::rows_fit(batch, q_len, q_heads)) return AMQ_ERR_UNSUPPORTED;
     if (batch == 0 || q_len == 0) return AMQ_OK;
     if (!q || !out || !lengths || (max_pages > 0 && !table)) return AMQ_ERR_INVALID_ARG;
     if (pages > 0 && (!cache_kcodes || !cache_kcoeffs || !cache_vcodes || !cache_vcoeffs)) return AMQ_ERR_INVALID_ARG;
