@@ -216,7 +216,7 @@ PyObject* py_binary_gemm_act(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         const amq_status s = p_amq_binary_gemm_act(
             static_cast<const uint32_t*>(Wc->data_ptr()), static_cast<const float*>(Wa->data_ptr()), (int)fits(m), (int)fits(n), (int)kw,
             static_cast<const uint32_t*>(xc->data_ptr()), static_cast<const float*>(xb->data_ptr()), (int)fits(batch), (int)ka,
-            bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, (int)act, residual ? static_cast<const float*>(residual->data_ptr()) : nullptr,
+            bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, act == (int)act ? (int)act : -1, residual ? static_cast<const float*>(residual->data_ptr()) : nullptr,
             residual ? (int)fits(leading(*residual)) : 0, static_cast<float*>(out.data_ptr()), (int)fits(leading(out)), on.stream());
         return s == AMQ_OK ? THPVariable_Wrap(out) : PyLong_FromLong(s);
     });
