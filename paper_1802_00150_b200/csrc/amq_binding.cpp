@@ -1,10 +1,11 @@
 // CPython binding of the C ABI in include/amq.h: argument marshalling only, in native code.
 //
 // A call through ctypes costs some 9 us of interpreter time (argument conversion, data_ptr per tensor, current_stream), twice a
-// short kernel's duration; here it costs about one.  Every entry point of the header is a Python function of the same name without the trailing
+// short kernel's duration; here it costs about one.  Entry points of the header are Python functions of the same name without the trailing
 // stream argument (the calling thread's current stream is used): pointers take None, a tensor (checked: CUDA, contiguous, the element
-// type of the pointer) or an integer address (unchecked: strided views, host memory), sizes take integers.  The library is opened
-// by path, so that an instrumented build can take its place.
+// type of the pointer) or an integer address (unchecked: strided views, host memory), sizes take integers.  The operators of a decoder step
+// take tensors instead, whose shapes and strides are looked at here (second half of this file).  The library is opened by path, so that an
+// instrumented build can take its place.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -64,11 +65,6 @@ struct Arg<T, std::enable_if_t<std::is_integral_v<T>>> {
     }
 };
 
-template <typename T>
-struct Arg<T, std::enable_if_t<std::is_floating_point_v<T>>> {
-    static T get(PyObject* o, Py_ssize_t) { return static_cast<T>(PyFloat_AsDouble(o)); }
-};
-
 template <typename... A, size_t... I>
 PyObject* call_checked(amq_status (*f)(A...), PyObject* const* args, std::index_sequence<I...>)
 {
@@ -104,10 +100,10 @@ PyObject* call(amq_status (*f)(A...), PyObject* const* args, Py_ssize_t nargs)
 }
 
 #define AMQ_ENTRIES(X)                                                                                                          \
-    X(amq_quantize) X(amq_pack) X(amq_unpack) X(amq_binary_dots) X(amq_binary_gemm) X(amq_binary_gemm_act) X(amq_quantized_gemv) X(amq_lstm_step)      \
+    X(amq_quantize) X(amq_pack) X(amq_unpack) X(amq_binary_dots) X(amq_binary_gemm) X(amq_quantized_gemv) X(amq_lstm_step)      \
     X(amq_lstm_step_static) X(amq_gru_step) X(amq_lstm_sequence) X(amq_gru_sequence) X(amq_lstm_sequence_host)                  \
     X(amq_gru_sequence_host) X(amq_selftest_sequence_give_up) X(amq_selftest_batched_sequence) X(amq_selftest_decode_give_up) X(amq_selftest_binary_gemm) \
-    X(amq_gru_step_original) X(amq_quantize_variant) X(amq_lm_greedy_decode) X(amq_log_softmax_argmax) X(amq_beam_select) X(amq_cache_append) X(amq_cache_attention) X(amq_embedding_rows) X(amq_lstm_step_paper) X(amq_lstm_sequence_paper)
+    X(amq_gru_step_original) X(amq_quantize_variant) X(amq_lm_greedy_decode) X(amq_log_softmax_argmax) X(amq_beam_select) X(amq_embedding_rows) X(amq_lstm_step_paper) X(amq_lstm_sequence_paper)
 
 #define AMQ_WRAP(name)                                                                          \
     decltype(&::name) p_##name = nullptr;                                                       \
@@ -182,6 +178,8 @@ struct On {
     void* stream() const { return c10::cuda::getCurrentCUDAStream().stream(); }
 };
 
+decltype(&::amq_binary_gemm_act) p_amq_binary_gemm_act = nullptr;
+
 // binary_gemm_act(Wcodes, Walpha, xcodes, xbeta, n, bias, activation, residual, y)
 PyObject* py_binary_gemm_act(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -255,6 +253,8 @@ bool cache_of(PyObject* cache, PyObject* table, PyObject* lengths, int64_t d, Ca
 
 template <typename T> T* data(const at::Tensor* t) { return static_cast<T*>(t->data_ptr()); }
 
+decltype(&::amq_cache_append) p_amq_cache_append = nullptr;
+
 // cache_append(kcodes, kcoeffs, vcodes, vcoeffs, cache, table, lengths, d)
 PyObject* py_cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -281,6 +281,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     });
 }
 
+decltype(&::amq_cache_attention) p_amq_cache_attention = nullptr;
 decltype(&::amq_cache_attention_workspace_bytes) p_amq_cache_attention_workspace_bytes = nullptr;
 
 // cache_attention(q, cache, table, lengths, scale, workspace, out)
@@ -461,6 +462,9 @@ PyObject* py_open(PyObject*, PyObject* path)
     p_##name = reinterpret_cast<decltype(&::name)>(dlsym(lib, #name));                          \
     if (!p_##name) { PyErr_SetString(PyExc_ImportError, "missing entry point " #name); return nullptr; }
     AMQ_ENTRIES(AMQ_LOOKUP)
+    AMQ_LOOKUP(amq_binary_gemm_act)
+    AMQ_LOOKUP(amq_cache_append)
+    AMQ_LOOKUP(amq_cache_attention)
     AMQ_LOOKUP(amq_beam_reorder)
     AMQ_LOOKUP(amq_cache_attention_workspace_bytes)
     Py_RETURN_NONE;
