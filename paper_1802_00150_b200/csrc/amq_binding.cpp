@@ -171,6 +171,18 @@ PyObject* guarded(F&& f)
     }
 }
 
+// The library's call without the interpreter's lock (a launch waits where the device's queue is full).  Its arguments are numbers and addresses, made before
+// the lock goes: other threads may change a list of tensors meanwhile.
+template <typename... P, typename... A>
+amq_status unlocked(amq_status (*f)(P...), A... args)
+{
+    amq_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = f(args...);
+    Py_END_ALLOW_THREADS
+    return s;
+}
+
 // the device of the call's tensors made current, and its current stream
 struct On {
     c10::cuda::CUDAGuard guard;
@@ -211,8 +223,8 @@ PyObject* py_binary_gemm_act(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         if (!same_device({Wc, Wa, xc, xb, bias, residual, y})) return nullptr;
         const On on(*Wc);
         at::Tensor out = y ? *y : fresh({batch, m}, at::kFloat, *Wc);
-        const amq_status s = p_amq_binary_gemm_act(
-            static_cast<const uint32_t*>(Wc->data_ptr()), static_cast<const float*>(Wa->data_ptr()), (int)fits(m), (int)fits(n), (int)kw,
+        const amq_status s = unlocked(
+            p_amq_binary_gemm_act, static_cast<const uint32_t*>(Wc->data_ptr()), static_cast<const float*>(Wa->data_ptr()), (int)fits(m), (int)fits(n), (int)kw,
             static_cast<const uint32_t*>(xc->data_ptr()), static_cast<const float*>(xb->data_ptr()), (int)fits(batch), (int)ka,
             bias ? static_cast<const float*>(bias->data_ptr()) : nullptr, act == (int)act ? (int)act : -1, residual ? static_cast<const float*>(residual->data_ptr()) : nullptr,
             residual ? (int)fits(leading(*residual)) : 0, static_cast<float*>(out.data_ptr()), (int)fits(leading(out)), on.stream());
@@ -273,7 +285,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         }
         if (!same_device({c.t[0], rows[0], rows[1], rows[2], rows[3]})) return nullptr;
         const On on(*c.t[0]);
-        return PyLong_FromLong(p_amq_cache_append(data<const uint32_t>(rows[0]), data<const float>(rows[1]), data<const uint32_t>(rows[2]), data<const float>(rows[3]),
+        return PyLong_FromLong(unlocked(p_amq_cache_append, data<const uint32_t>(rows[0]), data<const float>(rows[1]), data<const uint32_t>(rows[2]), data<const float>(rows[3]),
                                                   data<uint32_t>(c.t[0]), data<float>(c.t[1]), data<uint32_t>(c.t[2]), data<float>(c.t[3]),
                                                   (int)fits(c.pages), (int)fits(c.page_size), (int)fits(c.heads), (int)fits(d), (int)c.k, data<const int32_t>(c.table),
                                                   (int)fits(c.ld_table), (int)fits(c.max_pages), data<const int32_t>(c.lengths), (int)fits(c.batch), (int)fits(count),
@@ -314,8 +326,8 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs)
                                                                        (int)fits(c.max_pages * c.page_size));
             if (bytes) { own = fresh({(int64_t)bytes}, at::kByte, *q); workspace = &own; }
         }
-        const amq_status s = p_amq_cache_attention(
-            data<const float>(q), q->stride(0), q->stride(1), q->stride(2), data<const uint32_t>(c.t[0]), data<const float>(c.t[1]), data<const uint32_t>(c.t[2]),
+        const amq_status s = unlocked(
+            p_amq_cache_attention, data<const float>(q), q->stride(0), q->stride(1), q->stride(2), data<const uint32_t>(c.t[0]), data<const float>(c.t[1]), data<const uint32_t>(c.t[2]),
             data<const float>(c.t[3]), (int)fits(c.pages), (int)fits(c.page_size), (int)fits(c.heads), (int)fits(d), (int)c.k, data<const int32_t>(c.table),
             (int)fits(c.ld_table), (int)fits(c.max_pages), data<const int32_t>(c.lengths), (int)fits(batch), (int)fits(q_len), (int)fits(q_heads), scale,
             static_cast<float*>(out.data_ptr()), workspace ? workspace->data_ptr() : nullptr, workspace ? workspace->nbytes() : 0, on.stream());
@@ -356,7 +368,7 @@ PyObject* py_beam_select(PyObject*, PyObject* const* args, Py_ssize_t nargs)
         const int64_t n = batch * beams, step = (n + 3) / 4 * 4;         // (each part on 16 bytes)
         at::Tensor buffer = fresh({4 * step}, at::kInt, *scores);
         int32_t* at = static_cast<int32_t*>(buffer.data_ptr());
-        const amq_status s = p_amq_beam_select(data<const float>(logits), (int)fits(leading(*logits)), (int)fits(logits->size(1)), data<const float>(scores),
+        const amq_status s = unlocked(p_amq_beam_select, data<const float>(logits), (int)fits(leading(*logits)), (int)fits(logits->size(1)), data<const float>(scores),
                                                finished ? data<const int32_t>(finished) : nullptr, eos == (int)eos ? (int)eos : -2, (int)fits(batch), (int)fits(beams),
                                                reinterpret_cast<float*>(at), at + step, at + 2 * step, at + 3 * step, on.stream());
         if (s != AMQ_OK) return PyLong_FromLong(s);
@@ -432,13 +444,8 @@ PyObject* py_amq_beam_reorder(PyObject*, PyObject* const* args, Py_ssize_t nargs
                 }
                 if (ok) {
                     const On on(parents);
-                    void* stream = on.stream();
-                    amq_status s;
-                    Py_BEGIN_ALLOW_THREADS
-                    s = p_amq_beam_reorder(src, dst, bytes, from, to, (int)count, static_cast<const int32_t*>(parents.data_ptr()), (int)parents.size(0),
-                                           (int)parents.size(1), stream);
-                    Py_END_ALLOW_THREADS
-                    answer = PyLong_FromLong(s);
+                    answer = PyLong_FromLong(unlocked(p_amq_beam_reorder, src, dst, bytes, from, to, (int)count, static_cast<const int32_t*>(parents.data_ptr()),
+                                                      (int)parents.size(0), (int)parents.size(1), on.stream()));
                 }
             }
         }
