@@ -234,8 +234,8 @@ bgemm_resident_kernel(const __grid_constant__ ResGemmParams a)
                 if constexpr (POST) {
                     ok = __all_sync(0xffffffffu, mbar_wait_relaxed(smem_u32(&sy.yfull), y_parity, &sy.failed));
                     y_parity ^= 1u;
+                    asm volatile("cp.async.wait_all;" ::: "memory");        // (a wait that ran out leaves no copies in flight either)
                     if (!ok) { *(volatile int*)&sy.failed = 1; break; }
-                    asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll 4
                     for (int e = first; e < last; e += R::OUT_WARPS) {
                         float4 v = *reinterpret_cast<const float4*>(sY + e * Y_LD + 4 * lane);
