@@ -366,9 +366,10 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  *   out [batch][q_len][q_heads][d] fp32; batch * q_len * q_heads up to AMQ_MAX_TOKENS (else AMQ_ERR_UNSUPPORTED, and a workspace of 0 bytes).
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
  *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
- * Products with the planes are exact, on q and on p times coefficients held as 31-bit fixed-point numbers (relative to a query's largest element, and
- * to the largest weight and coefficient among those of 32 tokens that it sees; elements of a query below 2^-98 lose bits); everything else is fp32.  Results repeat
- * bit for bit for the same sizes and lengths.
+ * Products with the planes are exact, on numbers in fixed point: p times a value's coefficient has 31 bits relative to the largest weight and the largest
+ * coefficient among those of 32 tokens that the query sees; element j of a query has 31 - j % 8 bits, the sign among them, relative to the query's largest
+ * element (fewer where that is below 2^-98), so one far below the largest has fewer than fp32 gives it, as a sum in fp32 beside the largest would leave it.  Everything else is fp32.
+ * Results repeat bit for bit for the same sizes and lengths (the lengths of all sequences: they decide where sums are split).
  */
 AMQ_API size_t amq_cache_attention_workspace_bytes(int batch, int q_len, int q_heads, int heads, int d, int max_tokens);
 AMQ_API amq_status amq_cache_attention(const float* q, long long q_batch, long long q_token, long long q_head,
