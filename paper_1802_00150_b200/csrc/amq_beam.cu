@@ -44,6 +44,7 @@ __device__ __forceinline__ uint32_t ordered(float v)
     const uint32_t u = __float_as_uint(v + 0.0f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+constexpr uint32_t LOWEST = 0x00800000u;       // of -FLT_MAX
 __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
 
 // logits larger first, then tokens smaller first: one descending integer order
@@ -304,7 +305,9 @@ beam_select_kernel(SelectParams p)
             buffer ^= 1;
         }
         if (v && v >= bound) {
-            const float least = bound ? from_ordered(bound) : -3.402823466e38f;      // (no bound yet: everything but -inf)
+            // (a bound below every finite logit's is none: everything but -inf.  The bisection may end there, among the places of -inf and NaN, where a
+            // slice has few logits above the type's lowest value)
+            const float least = from_ordered(max(bound, LOWEST));
 #pragma unroll
             for (int i = 0; i < PT; ++i) {
                 if (now[i] >= least) {

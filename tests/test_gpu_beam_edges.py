@@ -128,3 +128,24 @@ def test_long_rows_of_equal_terms(amq, batch, beams, vocab):  # noqa: F811
         want = -(math.log(float(torch.exp(z - 1.5).sum())))
         assert (tokens[:, 0] == 0).all()
         assert (got[:, 0].double() - want).abs().max() <= bound + 2.0 ** -24 * abs(want)
+
+
+@pytest.mark.parametrize("batch", [1, 20, 70])
+@pytest.mark.parametrize("beams", [1, 4, 8, 9, 12, 20, 32])
+def test_few_tokens_above_the_lowest_value(amq, batch, beams):  # noqa: F811
+    """Tokens masked with the type's lowest value, up to all but a few of a row: the unmasked ones are found whatever their number, by that of the beams or below."""
+    gen = torch.Generator(device="cuda").manual_seed(beams)
+    for vocab in (31, 147, 402, 581, 3000):
+        for kept in (0.5, 0.1, 0.02):
+            z = torch.randn((batch * beams, vocab), device="cuda", generator=gen) * 2.5
+            z = torch.where(torch.rand(z.shape, device="cuda", generator=gen) < kept, z, LOWEST)
+            z[:, 3] = 1.0                                   # (one at least)
+            scores = -20 * torch.rand((batch, beams), device="cuda", generator=gen)
+            d = z.double()
+            top = d.amax(1, keepdim=True)
+            total = (d - top - torch.log(torch.exp(d - top).sum(1, keepdim=True))).view(batch, beams, vocab) + scores.double()[..., None]
+            best = torch.sort(total.view(batch, -1), dim=1, descending=True, stable=True)
+            got, parents, tokens, _ = amq.beam_select(z, scores)
+            assert ((got.double() - best.values[:, :beams]).abs() <= 2.0 ** -24 * best.values[:, :beams].abs() + 3e-6).all()
+            real = best.values[:, :beams] > -1e30           # (those of the lowest value differ by nothing that a double holds)
+            assert torch.equal((parents.long() * vocab + tokens)[real], best.indices[:, :beams][real])
