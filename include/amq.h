@@ -367,7 +367,7 @@ AMQ_API amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs
  *   workspace: DEVICE, amq_cache_attention_workspace_bytes(..) bytes (NULL where that is 0), 16-byte aligned, contents undefined between calls; not
  *   shared by calls that may run at the same time.  max_tokens = max_pages * page_size.
  * Products with the planes are exact, on numbers in fixed point: p times a value's coefficient has 31 bits relative to the largest weight and the largest
- * coefficient among those of 32 tokens that the query sees; element j of a query has 31 - j % 8 bits, the sign among them, relative to the query's largest
+ * coefficient among those of 32 tokens that the query sees (fewer where that is below 2^-97); element j of a query has 31 - j % 8 bits, the sign among them, relative to the query's largest
  * element (fewer where that is below 2^-98), so one far below the largest has fewer than fp32 gives it, as a sum in fp32 beside the largest would leave it.  Everything else is fp32.
  * Results repeat bit for bit for the same sizes and lengths (the lengths of all sequences: they decide where sums are split).
  */

@@ -12,9 +12,9 @@
 // sum does not depend on where it starts: equal rows get equal sums.  A lower bound of the share's K-th largest logit comes from the maxima of 32 or 64 groups
 // of threads, and little more than K logits reach it; those are written down, sorted by a warp, and go to the first CTA's shared memory, which
 // joins them by score.
-// Bound by instructions and barriers, 16 instructions for a lane and logit at 21 logits a thread and piece: load, maximum, exponential, sum, and some 240 a warp and
-// piece for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.5 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
-// one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 9 us, a chain of two barriers, the cluster's exchange and the join.
+// Bound by instructions and barriers, 17 instructions for a lane and logit at 21 logits a thread and piece: load, maximum, exponential, sum, and some 240 a warp and
+// piece for the bound, the candidates and the sums.  64 entries, 8 beams, 42000 tokens: 26.7 us, 3.2 TB/s (a CTA to an entry, a pass for the sum and
+// one for each beam: 149 us); one entry, 5 beams, 9999 tokens: 7.3 us, a chain of two barriers, the cluster's exchange and the join.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -50,6 +50,8 @@ __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_flo
 // logits larger first, then tokens smaller first: one descending integer order
 __device__ __forceinline__ unsigned long long candidate(float v, int token) { return ((unsigned long long)ordered(v) << 32) | (uint32_t)~token; }
 
+// one instruction, within 2^-22 of itself: less than the roundings of a piece's sum; twice as exact, a double's worth of work on 512 x 42000 logits would take longer
+// than all the rest
 __device__ __forceinline__ float exp2_ftz(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 constexpr float LOG2E = 1.44269504f;
 

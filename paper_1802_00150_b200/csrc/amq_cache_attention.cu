@@ -98,6 +98,8 @@ __device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint32_t (&a)[4], ui
 // two sums as floats: integers of up to 22 bits on top of MAGIC
 __device__ __forceinline__ f32x2 sums2(int a, int b) { return add2(pack2(__int_as_float(a), __int_as_float(b)), pack2(-MAGIC, -MAGIC)); }
 
+// One instruction, within 2^-22 of itself, as exp2f is not: a weight's error then is that of its score (whose fp32 sum of some hundred terms is off by as much
+// and more), and exp2f would add instructions to a kernel that is bound by them.
 __device__ __forceinline__ float exp2_approx(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 __device__ __forceinline__ int tiles_of(const CacheView& c, int b) { const int n = visible_length(c, b); return n > 0 ? (n - 1) / TILE + 1 : 0; }
@@ -151,9 +153,9 @@ __device__ __forceinline__ int sequence_at(const AttentionParams& p, long long x
 // digits, so that four query rows fill the 16 rows of an instruction, and the product is exact:
 //   q = sum_digits 256^i d_i (31-bit fixed point; elements whose bits lie at position j of a byte are held divided by 2^j),
 //   q . b = 2 sum_{bit = 1} q - sum q.
-// What bounds the kernel is the issue of instructions: for 8 tokens of 4 bits 33 MMAs, each of which holds a scheduler for 8 clocks whatever else could
-// issue (2.0 clocks of an SM alone, 3.2 with two ANDs beside it), and 300 others (64 AND, 36 byte permutations, 60 two-wide fp32, 36 of shared memory, 12 of
-// exponentials and conversions), against 1280 bytes.  64 sequences of 1024 to 4096 tokens, 8 heads, 32 query heads, d = 128, 4 bits: 112 us, 1.9 TB/s
+// What bounds the kernel is the issue of instructions: for 8 tokens of 4 bits 33 MMAs, each of which takes 2.2 clocks of an SM, 8.8 of a scheduler, and hides
+// half at most of what stands beside it (3.3 with two logic and four fp32 instructions, which alone take 2.0), and 300 others (64 AND, 36 byte permutations, 60 two-wide fp32, 36 of shared memory, 12 of
+// exponentials and conversions), against 1280 bytes.  64 sequences of 1024 to 4096 tokens, 8 heads, 32 query heads, d = 128, 4 bits: 111 us, 1.9 TB/s
 // (plain kernel, a CTA to a query row: 3346 us).  With the products on tcgen05 (kind::i8: keys' bytes in tensor memory, values' in shared memory, dimensions
 // contiguous) the same took 167 us: 7060 instructions for 128 tokens, nearly as many, and a chain of 5800 clocks from scores to results.
 //
@@ -164,7 +166,8 @@ __device__ __forceinline__ int sequence_at(const AttentionParams& p, long long x
 // word of the plane; results are those of tokens 2 c, 2 c + 1.  For values, c stands for the same two tokens, so weights never change
 // lanes, and column g for dimensions 16 g .. 16 g + 15, one per MMA.
 //
-// MT: row tiles of a CTA; what is done with the planes is done once for all of them.  WARPS: of a CTA.
+// MT: row tiles of a CTA; what is done with the planes is done once for all of them.  WARPS: of a CTA.  (Four warps, one row tile: 128 registers for four CTAs an SM;
+// at 4 bits 88 bytes of them are spilled, at 2 and 3 some 25.)
 template <int K, int MT, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, WARPS > 4 ? 1 : MT == 1 ? 4 : 2)
 cache_attention_kernel(const __grid_constant__ AttentionParams p)
