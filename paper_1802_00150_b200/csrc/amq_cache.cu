@@ -60,7 +60,7 @@ amq_status amq_cache_append(const uint32_t* kcodes, const float* kcoeffs, const 
     if (s != AMQ_OK) return s;
     if (batch < 0 || count < 0) return AMQ_ERR_INVALID_ARG;
     if ((long long)batch * count > 0x7fffffffll) return AMQ_ERR_UNSUPPORTED;
-    if (batch == 0 || count == 0 || max_pages == 0) return AMQ_OK;
+    if (batch == 0 || count == 0 || max_pages == 0 || pages == 0) return AMQ_OK;       // (no page: every row is left out)
     if (!kcodes || !kcoeffs || !vcodes || !vcoeffs || !table || !lengths || !cache_kcodes || !cache_kcoeffs || !cache_vcodes || !cache_vcoeffs)
         return AMQ_ERR_INVALID_ARG;
     if (!amq::aligned16(kcodes) || !amq::aligned16(vcodes) || !amq::aligned16(cache_kcodes) || !amq::aligned16(cache_vcodes)) return AMQ_ERR_ALIGNMENT;

@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from test_operator_arguments import ATTENTION, UNSUPPORTED, call, lib  # noqa: F401
+from test_operator_arguments import APPEND, ATTENTION, OK, UNSUPPORTED, call, lib, pointer  # noqa: F401
 
 MOST = 0x7fffff00
 
@@ -30,3 +30,9 @@ def test_the_largest_workspaces(lib):  # noqa: F811
         rows = q_len * q_heads // heads
         blocks = heads * ((rows + 3) // 4)
         assert 0 < size(batch, q_len, q_heads, heads, 128, MOST) <= max(blocks, 592) * 2 * 8 * (128 * 4 + 8)
+
+
+def test_append_to_a_cache_without_pages(lib):  # noqa: F811
+    """Rows on no page are left out: all of them, and a cache without pages has no addresses."""
+    none = {"cache_" + part: pointer(0) for part in ("kcodes", "kcoeffs", "vcodes", "vcoeffs")}
+    assert call(lib.amq_cache_append, APPEND, pages=0, **none) == OK
